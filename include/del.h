@@ -324,6 +324,92 @@ int del_get_kernel_times(del_ctx *ctx, double *ms, int64_t *launches, double *by
 int del_head_argmax_static(const void *x, const void *lm_head, int rows, int vocab, int d_model, int32_t *tokens,
                            void *cuda_stream);
 
+/* ---- Branching decoding over a paged cache: operators without a context
+ * They work on pages in the layout of del_kv, whoever owns them: a context's, or a cache of the caller's own.  Each call is one or two
+ * kernel launches on cuda_stream (async), allocates nothing, keeps nothing between calls, can be captured into a CUDA graph and
+ * needs the stream's device to be current.  All pointers are DEVICE memory, structs are read before the call returns.
+ * Positions, page tables and counts are read on the device; what is out of range there is skipped as said with each call, never
+ * followed.  What the host can see is checked: DEL_EINVAL (null or misaligned pointers, shapes), DEL_ECUDA (launch failed). */
+
+typedef struct {
+    void *k_pages, *v_pages;      /* bf16, 16-byte aligned; layouts as in del_kv */
+    int32_t n_pages, n_layers, n_kv_heads, head_dim;   /* head_dim 64 or 128; pages of 16 positions */
+} del_pages;
+
+/* Attention of a tree of drafted tokens over the paged cache, one layer.  Sequence b has lens[b] committed positions and
+ * nodes[b] <= max_nodes tree nodes, whose keys and values lie in the cache at positions lens[b] + i.  Node i sees all committed positions
+ * and the nodes j < nodes[b] with bit j of mask[b][i] set (itself only if its bit is set); its output for each query head is the
+ * softmax-weighted sum of the visible values, scores scale * q.k.  With max_nodes = 1 and mask = null: attention of single tokens.
+ *   - a row that sees nothing gets zeros; output rows i >= nodes[b] are left as they were;
+ *   - masked positions never contribute, whatever their pages hold; positions behind the table's columns or on a page id outside
+ *     [0, n_pages) are masked; lens and nodes below 0 count as 0, nodes above max_nodes as max_nodes;
+ *   - products bf16 x bf16 with fp32 sums; softmax in fp32; probabilities rounded to bf16 for the product with the values. */
+typedef struct {
+    const void *q;                /* bf16 [batch][max_nodes][n_heads][head_dim], rows q_node_stride apart, sequences q_seq_stride */
+    void *out, *out_lo;           /* bf16, like q; out_lo (may be null) gets the low part: out + out_lo carries 16 bits of mantissa */
+    const int32_t *page_table;    /* [batch] rows of table_cols entries, table_stride apart */
+    const int32_t *lens, *nodes;  /* [batch]; nodes may be null: max_nodes everywhere */
+    const uint64_t *mask;         /* [batch][max_nodes], may be null: a chain, node i sees nodes 0..i */
+    int64_t q_seq_stride, q_node_stride, out_seq_stride, out_node_stride;   /* in elements, multiples of 8 */
+    int32_t batch, max_nodes, n_heads;       /* max_nodes 1..64, n_heads a multiple of n_kv_heads, batch 1..65535 */
+    int32_t layer;                /* 1-based */
+    int32_t table_cols, table_stride;
+    int32_t max_len;              /* what lens are expected to reach (0: table_cols * 16): splits the work, changes no result but for the order of sums */
+    float scale;                  /* of the scores; 0: 1 / sqrt(head_dim) */
+} del_tree_attn;
+int del_tree_attention(const del_pages *kv, const del_tree_attn *args, void *cuda_stream);
+
+/* Moves cached positions of all layers and heads: position dst_start[b] + i of dst_table's row b becomes position src_pos[b][i] of
+ * src_table's row b, for i < counts[b] (at most max_count).  Commits the accepted path of a draft tree (src_table = dst_table,
+ * src_pos = lens + path, dst_start = lens), or compacts the kept positions of a context into other pages.  A row's sources and
+ * destinations may overlap if src_pos[b] ascends strictly and src_pos[b][i] >= dst_start[b] + i; otherwise no position written may be
+ * one that is read, nor may two rows write the same one.  A position outside its table (src_cols * 16, dst_cols * 16) or on a
+ * page id outside [0, n_pages) is not moved. */
+typedef struct {
+    const int32_t *src_table, *dst_table;    /* [batch] rows of src_cols / dst_cols entries, src_stride / dst_stride apart */
+    const int32_t *src_pos;                  /* [batch][max_count], rows pos_stride apart */
+    const int32_t *counts, *dst_start;       /* [batch] */
+    int32_t batch, max_count, src_cols, src_stride, dst_cols, dst_stride, pos_stride;
+} del_compact;
+int del_kv_compact(const del_pages *kv, const del_compact *args, void *cuda_stream);
+
+/* Forks, reorders and gives up rows (beams, samples) that share pages.  New row b continues old row a = parents[b]: new_lens[b] =
+ * lens[a], full pages are shared, and a part-filled last page stays with the lowest b of the parent while the others get copies in
+ * spare pages.  Then each row gets pages for `room` more positions (within new_cols).  Spare pages are taken in order,
+ * rows ascending, a row's copy first.  parents[b] outside [0, n_old): the row is given up, new_lens[b] = 0, no page.
+ *   - entries of new_table behind a row's pages are left as they were; new_table and new_lens must not overlap table and lens;
+ *   - spare (n_spare[0] <= spare_cap ids, DEVICE): pages that no row holds.  Where they run out, or where the parent's or the spare page's
+ *     id is outside [0, n_pages), the entry becomes -1 and counts[1] goes up by one;
+ *   - free_pages (may be null): the ids in [0, n_pages) that no new row holds, ascending, counts[0] of them, the rest of the array
+ *     left as it was; it holds n_pages entries, may not overlap spare, and serves as the next call's spare with n_spare = counts.
+ * 1 <= n_old, n_new <= 1024; with free_pages n_pages <= 1 << 20. */
+typedef struct {
+    const int32_t *table, *lens, *parents;   /* [n_old] rows of old_cols entries old_stride apart, [n_old], [n_new] */
+    const int32_t *spare, *n_spare;
+    int32_t *new_table, *new_lens;           /* [n_new] rows of new_cols entries new_stride apart, [n_new] */
+    int32_t *free_pages, *counts;            /* counts int32 [2]: free pages (0 if free_pages is null), pages missing */
+    int32_t n_old, n_new, old_cols, old_stride, new_cols, new_stride, spare_cap, room;
+} del_fork_args;
+int del_kv_fork(const del_pages *kv, const del_fork_args *args, void *cuda_stream);
+
+/* Beam search's selection: of every batch item the k best continuations over its beams and the vocabulary, by score
+ * scores[row] + log softmax(logits[row])[token], row = item * beams + beam.  Best first; equal scores: the lower row, then the higher
+ * logit, then the lower token id.  finished (may be null): a row with a non-zero entry has one continuation, token eos at its score
+ * unchanged.  A score that is no number below +inf counts as -inf (a row whose logits hold a NaN or +inf has only such);
+ * continuations at -inf are chosen last.  The order is taken in 64 bits, the log-sum-exp is accurate to fp32.
+ * 1 <= k <= 64, 1 <= beams <= 64, k <= beams * vocab, eos in [0, vocab) if finished is given. */
+enum { DEL_F32 = 0, DEL_BF16 = 1, DEL_F16 = 2 };
+typedef struct {
+    const void *logits;           /* [batch * beams] rows of vocab values of `dtype`, row_stride elements apart */
+    const float *scores;          /* [batch * beams] */
+    const uint8_t *finished;
+    float *out_scores;            /* [batch][k] */
+    int32_t *out_tokens, *out_rows;          /* [batch][k]; out_rows = item * beams + beam: the parents of del_kv_fork */
+    int64_t row_stride;
+    int32_t batch, beams, vocab, k, eos, dtype;
+} del_beam;
+int del_beam_select(const del_beam *args, void *cuda_stream);
+
 const char *del_strerror(int code);
 /* Text of the last CUDA error seen by this context ("" if none). */
 const char *del_last_cuda_error(const del_ctx *ctx);

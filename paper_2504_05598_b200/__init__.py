@@ -29,7 +29,8 @@ EXPORTS = ["del_workspace_bytes", "del_init", "del_prefill", "del_draft", "del_v
            "del_select", "del_round", "del_set_policy", "del_get_stats", "del_set_stats", "del_get_shadow",
            "del_get_drafts", "del_force_token", "del_get_hidden", "del_debug_logits", "del_get_kv", "del_committed_len", "del_release",
            "del_launch_count", "del_get_traffic", "del_set_flags", "del_get_kernel_times", "del_head_argmax_static",
-           "del_set_policy_fs", "del_set_exit_mode", "del_get_window", "del_set_sampling", "del_get_sample_info", "del_get_round_logits", "del_sample_probe", "del_get_conf_stats", "del_set_conf_stats", "del_get_conf", "del_debug_inject_error", "del_debug_routes", "del_strerror", "del_last_cuda_error", "del_destroy"]
+           "del_set_policy_fs", "del_set_exit_mode", "del_get_window", "del_set_sampling", "del_get_sample_info", "del_get_round_logits", "del_sample_probe", "del_get_conf_stats", "del_set_conf_stats", "del_get_conf", "del_debug_inject_error", "del_debug_routes",
+           "del_tree_attention", "del_kv_compact", "del_kv_fork", "del_beam_select", "del_strerror", "del_last_cuda_error", "del_destroy"]
 
 
 class Shape(C.Structure):
@@ -59,6 +60,33 @@ class RoundOut(C.Structure):
 
     def emitted(self) -> List[int]:
         return [int(self.tokens[i]) for i in range(self.n_emitted)]
+
+
+class Pages(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_layers", "n_kv_heads", "head_dim")]
+
+
+class TreeAttnC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "out_lo", "page_table", "lens", "nodes", "mask")] + \
+               [(n, C.c_int64) for n in ("q_seq_stride", "q_node_stride", "out_seq_stride", "out_node_stride")] + \
+               [(n, C.c_int32) for n in ("batch", "max_nodes", "n_heads", "layer", "table_cols", "table_stride", "max_len")] + \
+               [("scale", C.c_float)]
+
+
+class CompactC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("src_table", "dst_table", "src_pos", "counts", "dst_start")] + \
+               [(n, C.c_int32) for n in ("batch", "max_count", "src_cols", "src_stride", "dst_cols", "dst_stride", "pos_stride")]
+
+
+class ForkC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "lens", "parents", "spare", "n_spare", "new_table", "new_lens", "free_pages", "counts")] + \
+               [(n, C.c_int32) for n in ("n_old", "n_new", "old_cols", "old_stride", "new_cols", "new_stride", "spare_cap", "room")]
+
+
+class BeamC(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "scores", "finished", "out_scores", "out_tokens", "out_rows")] + \
+               [("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("batch", "beams", "vocab", "k", "eos", "dtype")]
 
 
 _lib = None
@@ -147,6 +175,11 @@ def load_library(build_if_missing: bool = True):
     L.del_get_kernel_times.argtypes = [vp, vp, vp, vp, ci]
     L.del_head_argmax_static.restype = ci
     L.del_head_argmax_static.argtypes = [vp, vp, ci, ci, ci, vp, vp]
+    for name, args in (("del_tree_attention", TreeAttnC), ("del_kv_compact", CompactC), ("del_kv_fork", ForkC)):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [C.POINTER(Pages), C.POINTER(args), vp]
+    L.del_beam_select.restype = ci
+    L.del_beam_select.argtypes = [C.POINTER(BeamC), vp]
     L.del_strerror.restype = C.c_char_p
     L.del_strerror.argtypes = [ci]
     L.del_last_cuda_error.restype = C.c_char_p
@@ -445,3 +478,143 @@ def head_argmax_static(x, lm_head, tokens_out, stream=None) -> int:
     st = stream or torch.cuda.current_stream(x.device)
     return load_library().del_head_argmax_static(x.data_ptr(), lm_head.data_ptr(), x.shape[0], lm_head.shape[0], x.shape[1],
                                                  tokens_out.data_ptr(), C.c_void_p(st.cuda_stream))
+
+
+# ---- branching decoding over a paged cache: operators without a context (include/del.h)
+def _refuse(what: str, why: str):
+    raise DelError(EINVAL, what, why)
+
+
+def _ints(what: str, name: str, t, dim: int, device):
+    """An int32 tensor of `dim` dimensions whose rows are contiguous, on the cache's device."""
+    if t.dtype is not _torch().int32 or t.dim() != dim or t.device != device or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        _refuse(what, f"{name}: int32, {dim}-dimensional, contiguous rows, on {device} expected")
+    return t.data_ptr()
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _pages(what: str, k_pages, v_pages):
+    """The cache's tensors [n_pages][n_layers][n_kv_heads][16][head_dim] / [...][head_dim][16] as the struct of the C call."""
+    bf16 = _torch().bfloat16
+    if k_pages.dtype is not bf16 or v_pages.dtype is not bf16 or not k_pages.is_cuda or v_pages.device != k_pages.device:
+        _refuse(what, "k_pages, v_pages: bf16 tensors on one CUDA device expected")
+    n, layers, nkv, ps, hd = k_pages.shape if k_pages.dim() == 5 else (0,) * 5
+    if ps != 16 or tuple(v_pages.shape) != (n, layers, nkv, hd, 16) or not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        _refuse(what, "k_pages [n][layers][kv heads][16][head_dim] and v_pages [n][layers][kv heads][head_dim][16], contiguous, expected")
+    return Pages(k_pages.data_ptr(), v_pages.data_ptr(), n, layers, nkv, hd)
+
+
+def _launch(what: str, device, stream, call):
+    """call(stream pointer) with the device current; raises on an error code."""
+    torch = _torch()
+    st = C.c_void_p((stream or torch.cuda.current_stream(device)).cuda_stream)
+    if torch.cuda.current_device() == device.index:
+        rc = call(st)
+    else:
+        with torch.cuda.device(device):
+            rc = call(st)
+    if rc != OK:
+        raise DelError(rc, what)
+
+
+def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None, mask=None, out=None, out_lo=None,
+                   scale: Optional[float] = None, max_len: int = 0, stream=None):
+    """del_tree_attention: attention of drafted trees (or single tokens) over a paged cache.
+
+    q: bf16 [batch, nodes, heads, head_dim], the last two dimensions contiguous; page_table int32 [batch, columns]; lens, nodes int32
+    [batch]; mask int64 [batch, nodes] (bit j of entry i: node i sees node j; None: a chain).  out (and out_lo, the low part of the result)
+    like q, made when None; returns out.  max_len: what lens are expected to reach."""
+    what, torch = "del_tree_attention", _torch()
+    kv = _pages(what, k_pages, v_pages)
+    dev = k_pages.device
+    if q.dim() != 4 or q.dtype is not torch.bfloat16 or q.device != dev or q.shape[3] != kv.head_dim:
+        _refuse(what, "q: bf16 [batch, nodes, heads, head_dim] on the cache's device expected")
+    batch, n, nh, hd = q.shape
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=dev)
+    for name, t in (("q", q), ("out", out), ("out_lo", out_lo)):
+        if t is not None and (t.shape != q.shape or t.dtype is not torch.bfloat16 or t.device != dev or t.stride(3) != 1 or (nh > 1 and t.stride(2) != hd)):
+            _refuse(what, f"{name}: bf16 like q, with contiguous rows of heads, expected")
+    if out_lo is not None and out_lo.stride() != out.stride():
+        _refuse(what, "out_lo: the strides of out expected")
+    if page_table.shape[0] != batch or lens.shape != (batch,) or (nodes is not None and nodes.shape != (batch,)):
+        _refuse(what, "page_table, lens, nodes: one row per sequence expected")
+    if mask is not None and (mask.dtype is not torch.int64 or mask.shape != (batch, n) or mask.device != dev or not mask.is_contiguous()):
+        _refuse(what, "mask: contiguous int64 [batch, nodes] expected")
+    if not lens.is_contiguous() or not (nodes is None or nodes.is_contiguous()):
+        _refuse(what, "lens, nodes: contiguous expected")
+    a = TreeAttnC(q.data_ptr(), out.data_ptr(), None if out_lo is None else out_lo.data_ptr(), _ints(what, "page_table", page_table, 2, dev),
+                  _ints(what, "lens", lens, 1, dev), None if nodes is None else _ints(what, "nodes", nodes, 1, dev),
+                  None if mask is None else mask.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
+                  batch, n, nh, layer, page_table.shape[1], page_table.stride(0), max_len, scale or 0.0)
+    lib = load_library()
+    _launch(what, dev, stream, lambda st: lib.del_tree_attention(kv, a, st))
+    return out
+
+
+def kv_compact(k_pages, v_pages, src_table, src_pos, counts, dst_table, dst_start, stream=None):
+    """del_kv_compact: position dst_start[b] + i of dst_table's row b becomes position src_pos[b, i] of src_table's row b, i < counts[b].
+
+    All int32: tables [batch, columns], src_pos [batch, max_count], counts and dst_start [batch]."""
+    what = "del_kv_compact"
+    kv = _pages(what, k_pages, v_pages)
+    dev, batch = k_pages.device, src_pos.shape[0]
+    if src_table.shape[0] != batch or dst_table.shape[0] != batch or counts.shape != (batch,) or dst_start.shape != (batch,):
+        _refuse(what, "one row per sequence expected")
+    a = CompactC(_ints(what, "src_table", src_table, 2, dev), _ints(what, "dst_table", dst_table, 2, dev), _ints(what, "src_pos", src_pos, 2, dev),
+                 _ints(what, "counts", counts, 1, dev), _ints(what, "dst_start", dst_start, 1, dev), batch, src_pos.shape[1],
+                 src_table.shape[1], src_table.stride(0), dst_table.shape[1], dst_table.stride(0), src_pos.stride(0))
+    lib = load_library()
+    _launch(what, dev, stream, lambda st: lib.del_kv_compact(kv, a, st))
+
+
+def kv_fork(k_pages, v_pages, table, lens, parents, spare, n_spare, new_table, new_lens, counts, room: int = 0, free_pages=None, stream=None):
+    """del_kv_fork: new row b continues old row parents[b], sharing its full pages; copies of part-filled pages and pages for `room`
+    more positions come from spare[:n_spare[0]].  Writes new_table, new_lens, counts (free pages, pages missing) and free_pages."""
+    what = "del_kv_fork"
+    kv = _pages(what, k_pages, v_pages)
+    dev = k_pages.device
+    if lens.shape[0] != table.shape[0] or new_table.shape[0] != parents.shape[0] or new_lens.shape != parents.shape:
+        _refuse(what, "lens one per row of table, new_table and new_lens one per parent expected")
+    if counts.shape != (2,) or n_spare.dim() != 1 or n_spare.shape[0] < 1 or (free_pages is not None and free_pages.shape != (kv.n_pages,)):
+        _refuse(what, "counts [2], n_spare [>= 1], free_pages [n_pages] expected")
+    a = ForkC(_ints(what, "table", table, 2, dev), _ints(what, "lens", lens, 1, dev), _ints(what, "parents", parents, 1, dev),
+              _ints(what, "spare", spare, 1, dev), _ints(what, "n_spare", n_spare, 1, dev), _ints(what, "new_table", new_table, 2, dev),
+              _ints(what, "new_lens", new_lens, 1, dev), None if free_pages is None else _ints(what, "free_pages", free_pages, 1, dev),
+              _ints(what, "counts", counts, 1, dev), table.shape[0], parents.shape[0], table.shape[1], table.stride(0), new_table.shape[1],
+              new_table.stride(0), spare.shape[0], room)
+    lib = load_library()
+    _launch(what, dev, stream, lambda st: lib.del_kv_fork(kv, a, st))
+
+
+def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None, eos: int = 0, stream=None):
+    """del_beam_select: the k best continuations of every item, k = out_scores.shape[1].
+
+    logits fp32, bf16 or fp16 [batch, beams, vocab] (equally spaced rows); scores fp32 [batch, beams]; finished bool [batch, beams];
+    out_scores fp32, out_tokens and out_rows int32 [batch, k].  out_rows = item * beams + beam."""
+    what, torch = "del_beam_select", _torch()
+    dtype = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(logits.dtype, -1)
+    dev = logits.device
+    if dtype < 0 or logits.dim() != 3 or not logits.is_cuda or (logits.shape[2] > 1 and logits.stride(2) != 1) or 0 in logits.shape:
+        _refuse(what, "logits: fp32, bf16 or fp16 [batch, beams, vocab] on a CUDA device expected")
+    batch, beams, vocab = logits.shape
+    row = logits.stride(1) if beams > 1 else max(logits.stride(0), vocab) if batch > 1 else vocab
+    if batch > 1 and logits.stride(0) != beams * row:
+        _refuse(what, "logits: equally spaced rows expected")
+    if scores.shape != (batch, beams) or scores.dtype is not torch.float32 or scores.device != dev or not scores.is_contiguous():
+        _refuse(what, "scores: contiguous fp32 [batch, beams] expected")
+    if finished is not None and (finished.shape != (batch, beams) or finished.dtype not in (torch.bool, torch.uint8) or finished.device != dev or not finished.is_contiguous()):
+        _refuse(what, "finished: contiguous bool [batch, beams] expected")
+    if out_scores.dtype is not torch.float32 or out_scores.dim() != 2 or out_scores.shape[0] != batch:
+        _refuse(what, "out_scores: fp32 [batch, k] expected")
+    for name, t, kind in (("out_scores", out_scores, torch.float32), ("out_tokens", out_tokens, torch.int32), ("out_rows", out_rows, torch.int32)):
+        if t.shape != out_scores.shape or t.dtype is not kind or t.device != dev or not t.is_contiguous():
+            _refuse(what, f"{name}: contiguous [batch, k] on the logits' device expected")
+    a = BeamC(logits.data_ptr(), scores.data_ptr(), None if finished is None else finished.data_ptr(), out_scores.data_ptr(),
+              out_tokens.data_ptr(), out_rows.data_ptr(), row, batch, beams, vocab, out_scores.shape[1], eos, dtype)
+    lib = load_library()
+    _launch(what, dev, stream, lambda st: lib.del_beam_select(a, st))

@@ -1,0 +1,52 @@
+// Device view of a paged cache handed to the context-free operators (del_pages), and the launch helper they share.
+#pragma once
+
+#include "../../include/del.h"
+#include "kernels.h"
+
+// keys [page][layer][kv head][16 tokens][hd], values [page][layer][kv head][hd][16 tokens]
+struct PageView {
+    bf16 *k, *v;
+    int32_t n_pages, L, nkv, hd;
+    __host__ __device__ size_t head_elems() const { return (size_t)16 * hd; }                 // of one (page, layer, head)
+    __host__ __device__ size_t page_elems() const { return (size_t)L * nkv * 16 * hd; }
+    __host__ __device__ bool holds(int page) const { return (unsigned)page < (unsigned)n_pages; }
+};
+
+// false: not a cache these operators take
+inline bool page_view(const del_pages *kv, PageView *v) {
+    if (!kv || !kv->k_pages || !kv->v_pages) return false;
+    if (((uintptr_t)kv->k_pages | (uintptr_t)kv->v_pages) & 15) return false;
+    if (kv->n_pages < 1 || kv->n_layers < 1 || kv->n_kv_heads < 1 || (kv->head_dim != 64 && kv->head_dim != 128)) return false;
+    if ((int64_t)kv->n_layers * kv->n_kv_heads > (1 << 20)) return false;
+    *v = PageView{(bf16 *)kv->k_pages, (bf16 *)kv->v_pages, kv->n_pages, kv->n_layers, kv->n_kv_heads, kv->head_dim};
+    return true;
+}
+
+// SMs of the current device (0: the query failed)
+inline int current_sms() {
+    static int n[DEL_MAX_DEVICES] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < DEL_MAX_DEVICES && n[dev]) return n[dev];
+    int sms = 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < DEL_MAX_DEVICES) n[dev] = sms;
+    return sms;
+}
+
+template <typename K, typename... A>
+inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, int cluster_x, cudaStream_t st, const A &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster_x;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster_x > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
