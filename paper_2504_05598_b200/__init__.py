@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct as _struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -68,7 +69,7 @@ class Pages(C.Structure):
 
 
 class TreeAttnC(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "out_lo", "page_table", "lens", "nodes", "mask")] + \
+    _fields_ = [(n, C.c_void_p) for n in ("q", "out", "out_lo", "page_table", "lens", "nodes", "mask", "error")] + \
                [(n, C.c_int64) for n in ("q_seq_stride", "q_node_stride", "out_seq_stride", "out_node_stride")] + \
                [(n, C.c_int32) for n in ("batch", "max_nodes", "n_heads", "layer", "table_cols", "table_stride", "max_len")] + \
                [("scale", C.c_float)]
@@ -90,6 +91,7 @@ class BeamC(C.Structure):
 
 
 _lib = None
+_t = None          # torch, once a tensor has been seen
 
 
 def load_library(build_if_missing: bool = True):
@@ -175,11 +177,11 @@ def load_library(build_if_missing: bool = True):
     L.del_get_kernel_times.argtypes = [vp, vp, vp, vp, ci]
     L.del_head_argmax_static.restype = ci
     L.del_head_argmax_static.argtypes = [vp, vp, ci, ci, ci, vp, vp]
-    for name, args in (("del_tree_attention", TreeAttnC), ("del_kv_compact", CompactC), ("del_kv_fork", ForkC)):
+    for name in ("del_tree_attention", "del_kv_compact", "del_kv_fork"):        # (structs: by reference, or packed as bytes)
         getattr(L, name).restype = ci
-        getattr(L, name).argtypes = [C.POINTER(Pages), C.POINTER(args), vp]
+        getattr(L, name).argtypes = [vp, vp, vp]
     L.del_beam_select.restype = ci
-    L.del_beam_select.argtypes = [C.POINTER(BeamC), vp]
+    L.del_beam_select.argtypes = [vp, vp]
     L.del_strerror.restype = C.c_char_p
     L.del_strerror.argtypes = [ci]
     L.del_last_cuda_error.restype = C.c_char_p
@@ -481,44 +483,68 @@ def head_argmax_static(x, lm_head, tokens_out, stream=None) -> int:
 
 
 # ---- branching decoding over a paged cache: operators without a context (include/del.h)
+# These calls are a few microseconds of GPU work in a loop over layers or steps: the checks below look at each tensor once, and
+# the C structs are packed as bytes (a ctypes structure of 24 fields takes 3 us to fill, packed bytes 1 us).
+_PACK_PAGES, _PACK_TREE = _struct.Struct("=2Q4i").pack, _struct.Struct("=8Q4q7if").pack
+_PACK_COMPACT, _PACK_FORK, _PACK_BEAM = _struct.Struct("=5Q7i4x").pack, _struct.Struct("=9Q8i").pack, _struct.Struct("=6Qq6i").pack
+
+
 def _refuse(what: str, why: str):
     raise DelError(EINVAL, what, why)
 
 
-def _ints(what: str, name: str, t, dim: int, device):
-    """An int32 tensor of `dim` dimensions whose rows are contiguous, on the cache's device."""
-    if t.dtype is not _torch().int32 or t.dim() != dim or t.device != device or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        _refuse(what, f"{name}: int32, {dim}-dimensional, contiguous rows, on {device} expected")
+def _vector(what: str, name: str, t, n: int, dev: int) -> int:
+    """Address of a contiguous int32 vector of n entries on that device."""
+    if t.dtype is not _t.int32 or t.dim() != 1 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        _refuse(what, f"{name}: contiguous int32 [{n}] on the cache's device expected")
     return t.data_ptr()
 
 
-def _torch():
-    import torch
-    return torch
+def _table(what: str, name: str, t, rows: int, dev: int):
+    """(address, columns, row stride) of an int32 matrix of that many rows, contiguous along them."""
+    if t.dtype is not _t.int32 or t.dim() != 2 or t.get_device() != dev:
+        _refuse(what, f"{name}: int32 [{rows}, columns] on the cache's device expected")
+    n, cols = t.shape
+    stride, one = t.stride()
+    if n != rows or cols < 1 or (cols > 1 and one != 1):
+        _refuse(what, f"{name}: int32 [{rows}, columns] with contiguous rows expected")
+    return t.data_ptr(), cols, stride
 
 
-def _pages(what: str, k_pages, v_pages):
-    """The cache's tensors [n_pages][n_layers][n_kv_heads][16][head_dim] / [...][head_dim][16] as the struct of the C call."""
-    bf16 = _torch().bfloat16
-    if k_pages.dtype is not bf16 or v_pages.dtype is not bf16 or not k_pages.is_cuda or v_pages.device != k_pages.device:
-        _refuse(what, "k_pages, v_pages: bf16 tensors on one CUDA device expected")
-    n, layers, nkv, ps, hd = k_pages.shape if k_pages.dim() == 5 else (0,) * 5
-    if ps != 16 or tuple(v_pages.shape) != (n, layers, nkv, hd, 16) or not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+def _pages(what: str, k, v):
+    """The cache's tensors [n_pages][n_layers][n_kv_heads][16][head_dim] / [...][head_dim][16]: (packed struct, pages, head_dim, device)."""
+    global _t
+    if _t is None:
+        import torch
+        _t = torch
+    bf16, dev = _t.bfloat16, k.get_device()
+    if k.dtype is not bf16 or v.dtype is not bf16 or dev < 0 or v.get_device() != dev or k.dim() != 5:
+        _refuse(what, "k_pages, v_pages: bf16 tensors of 5 dimensions on one CUDA device expected")
+    n, layers, heads, slots, hd = k.shape
+    if slots != 16 or v.shape != (n, layers, heads, hd, 16) or not (k.is_contiguous() and v.is_contiguous()):
         _refuse(what, "k_pages [n][layers][kv heads][16][head_dim] and v_pages [n][layers][kv heads][head_dim][16], contiguous, expected")
-    return Pages(k_pages.data_ptr(), v_pages.data_ptr(), n, layers, nkv, hd)
+    return _PACK_PAGES(k.data_ptr(), v.data_ptr(), n, layers, heads, hd), n, hd, dev
 
 
-def _launch(what: str, device, stream, call):
-    """call(stream pointer) with the device current; raises on an error code."""
-    torch = _torch()
-    st = C.c_void_p((stream or torch.cuda.current_stream(device)).cuda_stream)
-    if torch.cuda.current_device() == device.index:
-        rc = call(st)
+def _call(what: str, dev: int, fn, kv: bytes, args: bytes, stream):
+    """The C call on the stream (None: the device's current one) with the device current; raises on an error code."""
+    st = stream.cuda_stream if stream is not None else _t._C._cuda_getCurrentRawStream(dev)
+    if _t._C._cuda_getDevice() == dev:
+        rc = fn(kv, args, st) if kv is not None else fn(args, st)
     else:
-        with torch.cuda.device(device):
-            rc = call(st)
+        with _t.cuda.device(dev):
+            rc = fn(kv, args, st) if kv is not None else fn(args, st)
     if rc != OK:
         raise DelError(rc, what)
+
+
+def _rows_of_heads(what: str, name: str, t, shape, dev: int):
+    if t.dtype is not _t.bfloat16 or t.get_device() != dev or t.shape != shape:
+        _refuse(what, f"{name}: bf16 {list(shape)} on the cache's device expected")
+    seq, node, head, one = t.stride()
+    if one != 1 or (head != shape[3] and shape[2] > 1):
+        _refuse(what, f"{name}: the heads of a row contiguous expected")
+    return t.data_ptr(), seq, node
 
 
 def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None, mask=None, out=None, out_lo=None,
@@ -528,31 +554,31 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
     q: bf16 [batch, nodes, heads, head_dim], the last two dimensions contiguous; page_table int32 [batch, columns]; lens, nodes int32
     [batch]; mask int64 [batch, nodes] (bit j of entry i: node i sees node j; None: a chain).  out (and out_lo, the low part of the result)
     like q, made when None; returns out.  max_len: what lens are expected to reach."""
-    what, torch = "del_tree_attention", _torch()
-    kv = _pages(what, k_pages, v_pages)
-    dev = k_pages.device
-    if q.dim() != 4 or q.dtype is not torch.bfloat16 or q.device != dev or q.shape[3] != kv.head_dim:
-        _refuse(what, "q: bf16 [batch, nodes, heads, head_dim] on the cache's device expected")
-    batch, n, nh, hd = q.shape
+    what = "del_tree_attention"
+    kv, _, hd, dev = _pages(what, k_pages, v_pages)
+    shape = q.shape
+    if len(shape) != 4 or shape[3] != hd:
+        _refuse(what, "q: [batch, nodes, heads, head_dim] expected")
+    batch, n, nh, _ = shape
     if out is None:
-        out = torch.zeros(q.shape, dtype=q.dtype, device=dev)
-    for name, t in (("q", q), ("out", out), ("out_lo", out_lo)):
-        if t is not None and (t.shape != q.shape or t.dtype is not torch.bfloat16 or t.device != dev or t.stride(3) != 1 or (nh > 1 and t.stride(2) != hd)):
-            _refuse(what, f"{name}: bf16 like q, with contiguous rows of heads, expected")
-    if out_lo is not None and out_lo.stride() != out.stride():
-        _refuse(what, "out_lo: the strides of out expected")
-    if page_table.shape[0] != batch or lens.shape != (batch,) or (nodes is not None and nodes.shape != (batch,)):
-        _refuse(what, "page_table, lens, nodes: one row per sequence expected")
-    if mask is not None and (mask.dtype is not torch.int64 or mask.shape != (batch, n) or mask.device != dev or not mask.is_contiguous()):
-        _refuse(what, "mask: contiguous int64 [batch, nodes] expected")
-    if not lens.is_contiguous() or not (nodes is None or nodes.is_contiguous()):
-        _refuse(what, "lens, nodes: contiguous expected")
-    a = TreeAttnC(q.data_ptr(), out.data_ptr(), None if out_lo is None else out_lo.data_ptr(), _ints(what, "page_table", page_table, 2, dev),
-                  _ints(what, "lens", lens, 1, dev), None if nodes is None else _ints(what, "nodes", nodes, 1, dev),
-                  None if mask is None else mask.data_ptr(), q.stride(0), q.stride(1), out.stride(0), out.stride(1),
-                  batch, n, nh, layer, page_table.shape[1], page_table.stride(0), max_len, scale or 0.0)
-    lib = load_library()
-    _launch(what, dev, stream, lambda st: lib.del_tree_attention(kv, a, st))
+        out = _t.zeros(shape, dtype=_t.bfloat16, device=k_pages.device)
+    qp, q_seq, q_node = _rows_of_heads(what, "q", q, shape, dev)
+    op, o_seq, o_node = _rows_of_heads(what, "out", out, shape, dev)
+    lp = np_ = mp = 0
+    if out_lo is not None:
+        lp, l_seq, l_node = _rows_of_heads(what, "out_lo", out_lo, shape, dev)
+        if (l_seq, l_node) != (o_seq, o_node):
+            _refuse(what, "out_lo: the strides of out expected")
+    tp, cols, stride = _table(what, "page_table", page_table, batch, dev)
+    if nodes is not None:
+        np_ = _vector(what, "nodes", nodes, batch, dev)
+    if mask is not None:
+        if mask.dtype is not _t.int64 or mask.shape != (batch, n) or mask.get_device() != dev or not mask.is_contiguous():
+            _refuse(what, "mask: contiguous int64 [batch, nodes] on the cache's device expected")
+        mp = mask.data_ptr()
+    a = _PACK_TREE(qp, op, lp, tp, _vector(what, "lens", lens, batch, dev), np_, mp, 0, q_seq, q_node, o_seq, o_node, batch, n, nh, layer,
+                   cols, stride, max_len, scale or 0.0)
+    _call(what, dev, load_library().del_tree_attention, kv, a, stream)
     return out
 
 
@@ -561,34 +587,30 @@ def kv_compact(k_pages, v_pages, src_table, src_pos, counts, dst_table, dst_star
 
     All int32: tables [batch, columns], src_pos [batch, max_count], counts and dst_start [batch]."""
     what = "del_kv_compact"
-    kv = _pages(what, k_pages, v_pages)
-    dev, batch = k_pages.device, src_pos.shape[0]
-    if src_table.shape[0] != batch or dst_table.shape[0] != batch or counts.shape != (batch,) or dst_start.shape != (batch,):
-        _refuse(what, "one row per sequence expected")
-    a = CompactC(_ints(what, "src_table", src_table, 2, dev), _ints(what, "dst_table", dst_table, 2, dev), _ints(what, "src_pos", src_pos, 2, dev),
-                 _ints(what, "counts", counts, 1, dev), _ints(what, "dst_start", dst_start, 1, dev), batch, src_pos.shape[1],
-                 src_table.shape[1], src_table.stride(0), dst_table.shape[1], dst_table.stride(0), src_pos.stride(0))
-    lib = load_library()
-    _launch(what, dev, stream, lambda st: lib.del_kv_compact(kv, a, st))
+    kv, _, _, dev = _pages(what, k_pages, v_pages)
+    batch = src_pos.shape[0]
+    sp, s_cols, s_stride = _table(what, "src_table", src_table, batch, dev)
+    dp, d_cols, d_stride = _table(what, "dst_table", dst_table, batch, dev)
+    pp, most, p_stride = _table(what, "src_pos", src_pos, batch, dev)
+    a = _PACK_COMPACT(sp, dp, pp, _vector(what, "counts", counts, batch, dev), _vector(what, "dst_start", dst_start, batch, dev), batch, most,
+                      s_cols, s_stride, d_cols, d_stride, p_stride)
+    _call(what, dev, load_library().del_kv_compact, kv, a, stream)
 
 
 def kv_fork(k_pages, v_pages, table, lens, parents, spare, n_spare, new_table, new_lens, counts, room: int = 0, free_pages=None, stream=None):
     """del_kv_fork: new row b continues old row parents[b], sharing its full pages; copies of part-filled pages and pages for `room`
     more positions come from spare[:n_spare[0]].  Writes new_table, new_lens, counts (free pages, pages missing) and free_pages."""
     what = "del_kv_fork"
-    kv = _pages(what, k_pages, v_pages)
-    dev = k_pages.device
-    if lens.shape[0] != table.shape[0] or new_table.shape[0] != parents.shape[0] or new_lens.shape != parents.shape:
-        _refuse(what, "lens one per row of table, new_table and new_lens one per parent expected")
-    if counts.shape != (2,) or n_spare.dim() != 1 or n_spare.shape[0] < 1 or (free_pages is not None and free_pages.shape != (kv.n_pages,)):
-        _refuse(what, "counts [2], n_spare [>= 1], free_pages [n_pages] expected")
-    a = ForkC(_ints(what, "table", table, 2, dev), _ints(what, "lens", lens, 1, dev), _ints(what, "parents", parents, 1, dev),
-              _ints(what, "spare", spare, 1, dev), _ints(what, "n_spare", n_spare, 1, dev), _ints(what, "new_table", new_table, 2, dev),
-              _ints(what, "new_lens", new_lens, 1, dev), None if free_pages is None else _ints(what, "free_pages", free_pages, 1, dev),
-              _ints(what, "counts", counts, 1, dev), table.shape[0], parents.shape[0], table.shape[1], table.stride(0), new_table.shape[1],
-              new_table.stride(0), spare.shape[0], room)
-    lib = load_library()
-    _launch(what, dev, stream, lambda st: lib.del_kv_fork(kv, a, st))
+    kv, n_pages, _, dev = _pages(what, k_pages, v_pages)
+    n_old, n_new, n_listed = lens.numel(), parents.numel(), spare.numel()
+    tp, cols, stride = _table(what, "table", table, n_old, dev)
+    np_, new_cols, new_stride = _table(what, "new_table", new_table, n_new, dev)
+    a = _PACK_FORK(tp, _vector(what, "lens", lens, n_old, dev), _vector(what, "parents", parents, n_new, dev),
+                   _vector(what, "spare", spare, n_listed, dev), _vector(what, "n_spare", n_spare, n_spare.numel() or 1, dev), np_,
+                   _vector(what, "new_lens", new_lens, n_new, dev),
+                   0 if free_pages is None else _vector(what, "free_pages", free_pages, n_pages, dev), _vector(what, "counts", counts, 2, dev),
+                   n_old, n_new, cols, stride, new_cols, new_stride, n_listed, room)
+    _call(what, dev, load_library().del_kv_fork, kv, a, stream)
 
 
 def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None, eos: int = 0, stream=None):
@@ -596,25 +618,32 @@ def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None,
 
     logits fp32, bf16 or fp16 [batch, beams, vocab] (equally spaced rows); scores fp32 [batch, beams]; finished bool [batch, beams];
     out_scores fp32, out_tokens and out_rows int32 [batch, k].  out_rows = item * beams + beam."""
-    what, torch = "del_beam_select", _torch()
-    dtype = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(logits.dtype, -1)
-    dev = logits.device
-    if dtype < 0 or logits.dim() != 3 or not logits.is_cuda or (logits.shape[2] > 1 and logits.stride(2) != 1) or 0 in logits.shape:
+    global _t
+    if _t is None:
+        import torch
+        _t = torch
+    what, f32, shape, dev = "del_beam_select", _t.float32, logits.shape, logits.get_device()
+    dtype = 0 if logits.dtype is f32 else 1 if logits.dtype is _t.bfloat16 else 2 if logits.dtype is _t.float16 else -1
+    if dtype < 0 or len(shape) != 3 or dev < 0 or 0 in shape:
         _refuse(what, "logits: fp32, bf16 or fp16 [batch, beams, vocab] on a CUDA device expected")
-    batch, beams, vocab = logits.shape
-    row = logits.stride(1) if beams > 1 else max(logits.stride(0), vocab) if batch > 1 else vocab
-    if batch > 1 and logits.stride(0) != beams * row:
-        _refuse(what, "logits: equally spaced rows expected")
-    if scores.shape != (batch, beams) or scores.dtype is not torch.float32 or scores.device != dev or not scores.is_contiguous():
-        _refuse(what, "scores: contiguous fp32 [batch, beams] expected")
-    if finished is not None and (finished.shape != (batch, beams) or finished.dtype not in (torch.bool, torch.uint8) or finished.device != dev or not finished.is_contiguous()):
-        _refuse(what, "finished: contiguous bool [batch, beams] expected")
-    if out_scores.dtype is not torch.float32 or out_scores.dim() != 2 or out_scores.shape[0] != batch:
-        _refuse(what, "out_scores: fp32 [batch, k] expected")
-    for name, t, kind in (("out_scores", out_scores, torch.float32), ("out_tokens", out_tokens, torch.int32), ("out_rows", out_rows, torch.int32)):
-        if t.shape != out_scores.shape or t.dtype is not kind or t.device != dev or not t.is_contiguous():
-            _refuse(what, f"{name}: contiguous [batch, k] on the logits' device expected")
-    a = BeamC(logits.data_ptr(), scores.data_ptr(), None if finished is None else finished.data_ptr(), out_scores.data_ptr(),
-              out_tokens.data_ptr(), out_rows.data_ptr(), row, batch, beams, vocab, out_scores.shape[1], eos, dtype)
-    lib = load_library()
-    _launch(what, dev, stream, lambda st: lib.del_beam_select(a, st))
+    batch, beams, vocab = shape
+    st = logits.stride()
+    row = st[1] if beams > 1 else st[0] if batch > 1 else vocab
+    if (vocab > 1 and st[2] != 1) or (batch > 1 and st[0] != beams * row):
+        _refuse(what, "logits: equally spaced contiguous rows expected")
+    if scores.dtype is not f32 or scores.shape != (batch, beams) or scores.get_device() != dev or not scores.is_contiguous():
+        _refuse(what, "scores: contiguous fp32 [batch, beams] on the logits' device expected")
+    fp = 0
+    if finished is not None:
+        if finished.dtype not in (_t.bool, _t.uint8) or finished.shape != (batch, beams) or finished.get_device() != dev or not finished.is_contiguous():
+            _refuse(what, "finished: contiguous bool [batch, beams] on the logits' device expected")
+        fp = finished.data_ptr()
+    out = out_scores.shape
+    if len(out) != 2 or out[0] != batch or out_scores.dtype is not f32 or out_scores.get_device() != dev or not out_scores.is_contiguous():
+        _refuse(what, "out_scores: contiguous fp32 [batch, k] on the logits' device expected")
+    for t in (out_tokens, out_rows):
+        if t.shape != out or t.dtype is not _t.int32 or t.get_device() != dev or not t.is_contiguous():
+            _refuse(what, "out_tokens, out_rows: contiguous int32 [batch, k] on the logits' device expected")
+    a = _PACK_BEAM(logits.data_ptr(), scores.data_ptr(), fp, out_scores.data_ptr(), out_tokens.data_ptr(), out_rows.data_ptr(), row, batch,
+                   beams, vocab, out[1], eos, dtype)
+    _call(what, dev, load_library().del_beam_select, None, a, stream)

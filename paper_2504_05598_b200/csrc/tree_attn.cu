@@ -16,46 +16,16 @@
 #include <cooperative_groups.h>
 #include <cstring>
 
-#include "pages.cuh"
+#include "tree_attn.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace {
 
+using namespace tree;
+
 constexpr int NW = 8, THREADS = NW * 32, MAX_SPLITS = 16;
 constexpr float LOG2E = 1.4426950408889634f;
-
-struct TreeArgs {
-    PageView kv;
-    const bf16 *q;
-    bf16 *out, *out_lo;
-    const int32_t *table, *lens, *nodes;
-    const uint64_t *mask;
-    int64_t q_seq, q_node, o_seq, o_node;
-    int32_t max_nodes, nh, layer, cols, stride;
-    float scale;               // times log2(e)
-};
-
-// what a CTA knows of its sequence
-struct Seq {
-    int len, n, n_keys;        // committed positions, nodes, positions that may be seen (cut at the table's end)
-    const int32_t *pt;
-};
-
-__device__ __forceinline__ Seq load_seq(const TreeArgs &a, int b) {
-    Seq s;
-    const int cap = a.cols * 16;
-    s.len = min(max(a.lens[b], 0), cap);
-    s.n = a.nodes ? min(max(a.nodes[b], 0), a.max_nodes) : a.max_nodes;
-    s.n_keys = min(s.len + s.n, cap);
-    s.pt = a.table + (size_t)b * a.stride;
-    return s;
-}
-
-__device__ __forceinline__ bool sees(uint64_t bits, int tok, int len, int n_keys) {
-    const int j = tok - len;
-    return tok < n_keys && (j < 0 || ((bits >> j) & 1));       // (n_keys - len <= 64)
-}
 
 template <int HD>
 __global__ void __launch_bounds__(THREADS) tree_attention_kernel(const TreeArgs a) {
@@ -80,7 +50,7 @@ __global__ void __launch_bounds__(THREADS) tree_attention_kernel(const TreeArgs 
         const int rr = mt * 16 + g + 8 * h;
         rv[h] = rr < R;
         const int i = rv[h] ? rr / group : 0, hq = rv[h] ? rr - i * group : 0;
-        bits[h] = !rv[h] ? 0 : a.mask ? a.mask[(size_t)b * a.max_nodes + i] : (2ull << i) - 1;
+        bits[h] = rv[h] ? node_bits(a, b, i) : 0;
         const bf16 *qp = a.q + b * a.q_seq + i * a.q_node + (size_t)(kvh * group + hq) * HD + 8 * t;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[h][ks] = rv[h] ? *reinterpret_cast<const uint4 *>(qp + 32 * ks) : make_uint4(0, 0, 0, 0);
@@ -279,7 +249,7 @@ extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, v
     if (!x || !page_view(kv, &a.kv)) return DEL_EINVAL;
     if (!x->q || !x->out || !x->page_table || !x->lens) return DEL_EINVAL;
     if (((uintptr_t)x->q | (uintptr_t)x->out | (uintptr_t)x->out_lo) & 15) return DEL_EINVAL;
-    if (((uintptr_t)x->page_table | (uintptr_t)x->lens | (uintptr_t)x->nodes) & 3 || (uintptr_t)x->mask & 7) return DEL_EINVAL;
+    if (((uintptr_t)x->page_table | (uintptr_t)x->lens | (uintptr_t)x->nodes | (uintptr_t)x->error) & 3 || (uintptr_t)x->mask & 7) return DEL_EINVAL;
     if ((x->q_seq_stride | x->q_node_stride | x->out_seq_stride | x->out_node_stride) & 7) return DEL_EINVAL;
     if (x->batch < 1 || x->batch > 65535 || x->max_nodes < 1 || x->max_nodes > 64) return DEL_EINVAL;
     if (x->n_heads < 1 || x->n_heads % a.kv.nkv || x->layer < 1 || x->layer > a.kv.L) return DEL_EINVAL;
@@ -294,9 +264,12 @@ extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, v
     a.q_seq = x->q_seq_stride; a.q_node = x->q_node_stride; a.o_seq = x->out_seq_stride; a.o_node = x->out_node_stride;
     a.max_nodes = x->max_nodes; a.nh = x->n_heads; a.layer = x->layer; a.cols = x->table_cols; a.stride = x->table_stride;
     a.scale = (x->scale > 0.f ? x->scale : 1.f / sqrtf((float)a.kv.hd)) * LOG2E;
+    a.err = x->error;
     const int64_t units = tiles * a.kv.nkv * x->batch;
     const int len = x->max_len ? (x->max_len < x->table_cols * 16 ? x->max_len : x->table_cols * 16) : x->table_cols * 16;
     const int pages = (len + x->max_nodes + 15) / 16;
+    if (x->max_nodes * group > 16)
+        return launch_tree_attention_tc(a, x->batch, len, n_sms, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
     int splits = 1;
     while (splits < MAX_SPLITS && units * splits * 2 <= 2 * n_sms && pages > splits * NW) splits *= 2;
     cudaError_t e = a.kv.hd == 128 ? launch<128>(a, x->batch, splits, (cudaStream_t)cuda_stream)

@@ -25,7 +25,7 @@ def call(name, cls, good, over, pages=None):
     return getattr(lib, name)(C.byref(kv(**(pages or {}))), C.byref(a), None)
 
 
-TREE = dict(q=P, out=P, out_lo=None, page_table=P, lens=P, nodes=None, mask=None, q_seq_stride=512, q_node_stride=256, out_seq_stride=512,
+TREE = dict(q=P, out=P, out_lo=None, page_table=P, lens=P, nodes=None, mask=None, error=None, q_seq_stride=512, q_node_stride=256, out_seq_stride=512,
             out_node_stride=256, batch=1, max_nodes=2, n_heads=4, layer=1, table_cols=4, table_stride=4, max_len=0, scale=0.0)
 COMPACT = dict(src_table=P, dst_table=P, src_pos=P, counts=P, dst_start=P, batch=1, max_count=4, src_cols=4, src_stride=4, dst_cols=4,
                dst_stride=4, pos_stride=4)
