@@ -2,16 +2,20 @@
 //
 // One CTA = up to two tiles of 128 query rows (node x query head of the group) of one kv head of one sequence, and a contiguous part
 // of its keys; a cluster of CTAs covers all keys and joins its parts through distributed shared memory: one launch, no workspace.
-// Keys and values stream once through shared memory in blocks of 64 positions (four pages), whatever the number of rows: the key
+// Keys and values stream once through shared memory in blocks of 128 positions (eight pages), whatever the number of rows: the key
 // pages [16][hd] and the value pages [hd][16] are the K-major operand tiles tcgen05.mma wants, so TMA copies them as they lie (5-d maps
 // of the cache, 128-byte swizzle for keys, 32-byte swizzle for values).  Per block and tile:
-//   S = Q K^T      M 128, N 64, into one of two 64-column accumulators in tensor memory;
-//   softmax        one thread per query row: tcgen05.ld of its 64 scores, p = 2^(s - m) against a lazily raised reference m (the output in
-//                  tensor memory is rescaled only when the row maximum has grown by more than 2^8), p as bf16 into shared memory;
-//   O += P V       M 128, N hd, K 16 per page.
-// Roles: warp 0 issues the copies, warp 1 the MMAs (the scores of block j + 1 before the probabilities of block j are waited for),
-// four warps per tile do the softmax; quarters of a tile without rows do nothing.  Every mbarrier wait is bounded and gives up as soon as
-// another role has: the rows then become NaN and the caller's error word, if there is one, is set.
+//   S = Q K^T      M 128, N 128, into tensor memory;
+//   softmax        one thread per query row, two sweeps of tcgen05.ld over its 128 scores: their maximum; then p = 2^(s - m) against a
+//                  lazily raised reference m (the output in tensor memory is rescaled only when the row maximum has grown by more
+//                  than 2^8), written as bf16 over the scores;
+//   O += P V       M 128, N hd, K 16 per page, P read from tensor memory.
+// Shared memory's 128 bytes per clock are what the MMAs compete for: with N = 64 and P in shared memory, scores and products of a
+// block of 64 keys read 80 KB per tile (640 cycles, 256 of arithmetic); with N = 128 and P in tensor memory 48 KB.
+// Roles: warp 0 issues the copies, warp 1 the MMAs, four warps per tile do the softmax; quarters of a tile without rows do nothing.
+// With two tiles each has one score buffer and one tile's softmax runs beside the other's MMAs; a single tile has two buffers.
+// Every mbarrier wait is bounded and gives up as soon as another role has: the rows then become NaN and the caller's error word, if
+// there is one, is set.
 //
 // What is masked never enters a sum: scores by selection; values of drafted or never written slots are looked at, and where one is not
 // finite its token's column is zeroed in shared memory and added at the end to those rows that see it.
@@ -29,7 +33,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int BQ = 128, BKEY = 64;
+constexpr int BQ = 128, BKEY = 128, PAGES = BKEY / 16;
 constexpr float RESCALE_STEP = 8.f;              // log2 units
 
 template <int HD, int TILES>
@@ -37,15 +41,17 @@ struct Cfg {
     static constexpr int KB = HD / 64;                             // 64-dim k-blocks of a key or query row
     static constexpr int Q_PART = BQ * 128;                        // [128 rows][128 B]
     static constexpr int Q_BYTES = TILES * KB * Q_PART;
-    static constexpr int P_BYTES = TILES * BQ * 128;               // [128 rows][64 keys] bf16 each
-    static constexpr int K_BYTES = KB * BKEY * 128, V_BYTES = 4 * HD * 32, STAGE = K_BYTES + V_BYTES;
-    static constexpr int STAGES = HD == 128 ? (TILES == 2 ? 4 : 5) : 8;
-    static constexpr int O_BYTES = TILES * BQ * HD * 4;            // the parts' outputs, where the stages were
-    static constexpr int SMEM = Q_BYTES + P_BYTES + STAGES * STAGE + 1024;
+    static constexpr int K_BYTES = KB * BKEY * 128, V_BYTES = PAGES * HD * 32;
+    static constexpr int KS = HD == 128 ? (TILES == 2 ? 2 : 3) : 5, VS = HD == 128 ? 3 : 6;      // blocks in the rings
+    static constexpr int RING = KS * K_BYTES + VS * V_BYTES;
+    static constexpr int O_BYTES = TILES * BQ * HD * 4;            // the parts' outputs, where the rings were
+    static constexpr int SMEM = Q_BYTES + RING + 1024;
     static constexpr int THREADS = 64 + TILES * 128;
-    static constexpr uint32_t O_COL = TILES * 2 * BKEY;            // S buffers first, then the outputs
-    static constexpr uint32_t TMEM = O_COL + TILES * HD <= 256 ? 256 : 512;
-    static_assert(O_BYTES <= STAGES * STAGE, "outputs do not fit where the stages were");
+    static constexpr int BUFS = 2;                                 // score buffers: one per tile, or two of the only tile
+    static constexpr uint32_t O_COL = BUFS * BKEY;                 // score buffers first, then the outputs
+    static constexpr uint32_t TMEM = 512;
+    static_assert(O_BYTES <= RING, "outputs do not fit where the rings were");
+    static_assert(O_COL + TILES * HD <= TMEM, "too much tensor memory");
     static_assert(SMEM <= 232448 - 512, "too much shared memory");
 };
 
@@ -78,18 +84,39 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
                    "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
                  : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// the same product with A in tensor memory: lane = row, a 32-bit column holds two consecutive bf16 of k
+__device__ __forceinline__ void umma_bf16_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+                 ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2f(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// two lanes of fp32 arithmetic in one instruction
+__device__ __forceinline__ void fma2(float &x0, float &x1, float b, float c) {          // x = x * b + c
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(x0), "+f"(x1) : "f"(b), "f"(c));
+}
+__device__ __forceinline__ void add2(float &x0, float &x1, float b0, float b1) {        // x += b
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(b0), "f"(b1));
+}
 __device__ __forceinline__ bool odd_pair(uint32_t x) {             // either bf16 of the word is an infinity or no number
     return (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
 }
 
-// which of the block's 64 positions a row sees: bit e = position key0 + e
+// which of 64 positions from key0 on a row sees: bit e = position key0 + e
 __device__ __forceinline__ uint64_t visible(uint64_t bits, int key0, int len, int n_keys) {
-    const int c = len - key0;                                       // committed positions of the block and beyond it
+    const int c = len - key0;                                       // committed positions from key0 on
     uint64_t vm = c >= 64 ? ~0ull : c > 0 ? ((1ull << c) - 1) | (bits << c) : c > -64 ? bits >> -c : 0;
     const int left = n_keys - key0;
     if (left < 64) vm &= left > 0 ? (1ull << left) - 1 : 0;
@@ -100,13 +127,13 @@ template <int HD, int TILES>
 __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TreeArgs a) {
     using C = Cfg<HD, TILES>;
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) uint64_t q_full, kv_full[C::STAGES], kv_empty[C::STAGES], s_full[TILES][2], s_empty[TILES][2], p_full[TILES], o_done[TILES], tile_bar, all_bar;
+    __shared__ __align__(8) uint64_t q_full, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], s_full[2], p_full[2], o_done[TILES], tile_bar, all_bar;
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile int s_err;
     __shared__ int s_bad_page, s_odd[2];
     __shared__ unsigned long long s_odd_tokens;                     // drafted tokens whose values were zeroed
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
-    unsigned char *q_sm = base, *p_sm = base + C::Q_BYTES, *kv_sm = p_sm + C::P_BYTES;
+    unsigned char *q_sm = base, *k_sm = base + C::Q_BYTES, *v_sm = k_sm + C::KS * C::K_BYTES;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n_splits = gridDim.x, split = blockIdx.x, b = blockIdx.z;
@@ -117,7 +144,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     const int R = s.n * group;
     if (row0 >= R) return;                                          // (the whole cluster)
 
-    // this CTA's blocks of 64 positions
+    // this CTA's blocks of positions
     const int nb = (s.n_keys + BKEY - 1) / BKEY, per = (nb + n_splits - 1) / n_splits;
     const int kb0 = min(split * per, nb), n_kb = min(per, nb - kb0);
     const int n_pages = (s.n_keys + 15) >> 4;
@@ -125,18 +152,18 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     auto quarters = [&](int t) { return min(4, max(0, (R - row0 - t * BQ + 31) >> 5)); };      // of tile t, that have rows
     const int n_tiles = TILES == 2 && quarters(1) > 0 ? 2 : 1;
     const int n_warps = quarters(0) + (TILES == 2 ? quarters(TILES - 1) : 0);                  // softmax warps at work
-    auto part_ml = [&](unsigned char *p, int x) { return reinterpret_cast<float2 *>(p + (x >> 7) * BQ * 128 + (x & 127) * 8); };   // where the probabilities were
+    auto part_ml = [&](unsigned char *p, int x) { return reinterpret_cast<float2 *>(p + x * 8); };       // where the queries were
     if (threadIdx.x == 0) {
         mbar_init(&q_full, n_warps);
         mbar_init(&all_bar, n_warps);
-        mbar_init(&tile_bar, max(1, quarters(0)));
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(&kv_full[i], 1); mbar_init(&kv_empty[i], 1); }
-        for (int t = 0; t < TILES; ++t) {
-            const int nq = max(1, quarters(t));
-            for (int i = 0; i < 2; ++i) { mbar_init(&s_full[t][i], 1); mbar_init(&s_empty[t][i], nq); }
-            mbar_init(&p_full[t], nq);
-            mbar_init(&o_done[t], 1);
+        mbar_init(&tile_bar, quarters(0));
+        for (int i = 0; i < C::KS; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+        for (int i = 0; i < C::VS; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_full[i], TILES == 2 ? max(1, quarters(i)) : quarters(0));
         }
+        for (int t = 0; t < TILES; ++t) mbar_init(&o_done[t], 1);
         s_err = 0;
         s_bad_page = s_odd[0] = s_odd[1] = 0;
         s_odd_tokens = 0;
@@ -152,94 +179,107 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     const uint32_t tmem_base = tmem_base_s;
 
     if (warp == 0) {
-        // Page ids: lane i holds page i of the current eight blocks, the next eight are requested one round ahead.  A position
+        // Page ids: lane i holds page i of the current four blocks, the next four are requested one round ahead.  A position
         // behind the last, or an id that names no page, is copied from coordinate -1: zeros.
         auto page_of = [&](int pi) {
             const int pg = pi < n_pages ? s.pt[pi] : -1;
             return a.kv.holds(pg) ? pg : -1;
         };
-        int cur = page_of(4 * kb0 + lane), nxt = page_of(4 * kb0 + 32 + lane);
-        int j = 0;
-        for (; j < n_kb; ++j) {
-            const int st = j % C::STAGES, first = (4 * j) & 31;
-            if (first == 0 && j > 0) { cur = nxt; nxt = page_of(4 * (kb0 + j) + 32 + lane); }
-            int pages[4];
+        int cur = page_of(PAGES * kb0 + lane), nxt = page_of(PAGES * kb0 + 32 + lane);
+        int n_k = 0, n_v = 0;                        // blocks whose keys, whose values are on their way
+        for (int j = 0; j < n_kb; ++j) {
+            const int ks = j % C::KS, vs = j % C::VS, first = (PAGES * j) & 31;
+            if (first == 0 && j > 0) { cur = nxt; nxt = page_of(PAGES * (kb0 + j) + 32 + lane); }
+            int pages[PAGES];
 #pragma unroll
-            for (int pg = 0; pg < 4; ++pg) pages[pg] = __shfl_sync(0xffffffffu, cur, first + pg);
+            for (int pg = 0; pg < PAGES; ++pg) pages[pg] = __shfl_sync(0xffffffffu, cur, first + pg);
             bool ok = true;
             if (lane == 0) {
-                if (j >= C::STAGES && !wait_or_err(&kv_empty[st], ((j / C::STAGES) & 1) ^ 1, &s_err)) {
+                if (j >= C::KS && !wait_or_err(&k_empty[ks], ((j / C::KS) & 1) ^ 1, &s_err)) {
                     if (!s_err) s_err = 1;
                     ok = false;
                 } else {
-                    mbar_expect_tx(&kv_full[st], C::STAGE);
-                    unsigned char *kst = kv_sm + (size_t)st * C::STAGE, *vst = kst + C::K_BYTES;
+                    mbar_expect_tx(&k_full[ks], C::K_BYTES);
 #pragma unroll
-                    for (int pg = 0; pg < 4; ++pg) {
+                    for (int pg = 0; pg < PAGES; ++pg)
 #pragma unroll
                         for (int kb = 0; kb < C::KB; ++kb)
-                            tma_load_5d(kst + kb * BKEY * 128 + pg * 2048, &maps.k, kb * 64, 0, kvh, a.layer - 1, pages[pg], &kv_full[st]);
-                        tma_load_5d(vst + pg * HD * 32, &maps.v, 0, 0, kvh, a.layer - 1, pages[pg], &kv_full[st]);
-                    }
+                            tma_load_5d(k_sm + ks * C::K_BYTES + kb * BKEY * 128 + pg * 2048, &maps.k, kb * 64, 0, kvh, a.layer - 1, pages[pg], &k_full[ks]);
+                    n_k = j + 1;
+                }
+                if (ok && j >= C::VS && !wait_or_err(&v_empty[vs], ((j / C::VS) & 1) ^ 1, &s_err)) {
+                    if (!s_err) s_err = 2;
+                    ok = false;
+                } else if (ok) {
+                    mbar_expect_tx(&v_full[vs], C::V_BYTES);
+#pragma unroll
+                    for (int pg = 0; pg < PAGES; ++pg)
+                        tma_load_5d(v_sm + vs * C::V_BYTES + pg * HD * 32, &maps.v, 0, 0, kvh, a.layer - 1, pages[pg], &v_full[vs]);
+                    n_v = j + 1;
                 }
             }
             if (!__shfl_sync(0xffffffffu, (int)ok, 0)) break;
         }
-        if (s_err && lane == 0) drain(kv_full, C::STAGES, j % C::STAGES, (uint32_t)(j / C::STAGES) & 1);
+        if (s_err && lane == 0) {
+            drain(k_full, C::KS, n_k % C::KS, (uint32_t)(n_k / C::KS) & 1);
+            drain(v_full, C::VS, n_v % C::VS, (uint32_t)(n_v / C::VS) & 1);
+        }
     } else if (warp == 1) {
         if (lane == 0 && n_kb > 0) {
-            // instruction descriptors: fp32 accumulate, bf16 x bf16, both operands K-major, M = 128, N = 64 / HD
+            // instruction descriptors: fp32 accumulate, bf16 x bf16, both operands K-major, M = 128, N = 128 / HD
             const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BKEY >> 3) << 17) | ((uint32_t)(BQ >> 4) << 24);
             const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(HD >> 3) << 17) | ((uint32_t)(BQ >> 4) << 24);
-            const uint32_t q_addr = smem_u32(q_sm), p_addr = smem_u32(p_sm);
-            int n_s[TILES] = {}, n_o = 0;            // blocks whose scores of tile t, whose products with the values have been issued
+            const uint32_t q_addr = smem_u32(q_sm), k_addr = smem_u32(k_sm), v_addr = smem_u32(v_sm);
+            int n_s[2] = {0, 0}, n_p[2] = {0, 0}, n_v = 0, n_k = 0;   // scores issued into each buffer, products of each tile, blocks whose values, whose keys were given back
             bool ok = wait_or_err(&q_full, 0, &s_err);
-            if (!ok && !s_err) s_err = 2;
-            auto issue_scores = [&](int j) -> bool {
-                const int st = j % C::STAGES, buf = j & 1;
-                if (!wait_or_err(&kv_full[st], (j / C::STAGES) & 1, &s_err)) { if (!s_err) s_err = 3; return false; }
-                const uint32_t k_addr = smem_u32(kv_sm + (size_t)st * C::STAGE);
+            if (!ok && !s_err) s_err = 3;
+            // scores of block j, tile t, into buffer buf: whatever used the buffer before was issued earlier, and MMAs run in order
+            auto scores = [&](int j, int t, int buf) -> bool {
+                if (!wait_or_err(&k_full[j % C::KS], (j / C::KS) & 1, &s_err)) { if (!s_err) s_err = 4; return false; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    if (t >= n_tiles) break;
-                    if (j >= 2 && !wait_or_err(&s_empty[t][buf], ((j >> 1) & 1) ^ 1, &s_err)) { if (!s_err) s_err = 4; return false; }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t d_tmem = tmem_base + (uint32_t)((t * 2 + buf) * BKEY);
+                for (int kb = 0; kb < C::KB; ++kb) {
+                    const uint64_t da = umma_desc(q_addr + (t * C::KB + kb) * C::Q_PART), db = umma_desc(k_addr + (j % C::KS) * C::K_BYTES + kb * BKEY * 128);
 #pragma unroll
-                    for (int kb = 0; kb < C::KB; ++kb) {
-                        const uint64_t da = umma_desc(q_addr + (t * C::KB + kb) * C::Q_PART), db = umma_desc(k_addr + kb * BKEY * 128);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) umma_bf16(d_tmem, da + 2 * k, db + 2 * k, idesc_s, (kb | k) != 0);
-                    }
-                    umma_commit(&s_full[t][buf]);
-                    n_s[t] = j + 1;
+                    for (int k = 0; k < 4; ++k) umma_bf16(tmem_base + (uint32_t)(buf * BKEY), da + 2 * k, db + 2 * k, idesc_s, (kb | k) != 0);
                 }
+                umma_commit(&s_full[buf]);
+                ++n_s[buf];
+                if (t == n_tiles - 1) { umma_commit(&k_empty[j % C::KS]); n_k = j + 1; }
                 return true;
             };
-            if (ok) ok = issue_scores(0);
+            auto products = [&](int j, int t, int buf) -> bool {
+                if (!wait_or_err(&p_full[buf], (TILES == 2 ? j : j >> 1) & 1, &s_err)) { if (!s_err) s_err = 5; return false; }
+                if (t == 0 && !wait_or_err(&v_full[j % C::VS], (j / C::VS) & 1, &s_err)) { if (!s_err) s_err = 6; return false; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int kk = 0; kk < PAGES; ++kk)
+                    umma_bf16_ts(tmem_base + C::O_COL + (uint32_t)(t * HD), tmem_base + (uint32_t)(buf * BKEY + kk * 8),
+                                 umma_desc_sw32(v_addr + (j % C::VS) * C::V_BYTES + kk * HD * 32), idesc_o, (j | kk) != 0);
+                umma_commit(&o_done[t]);
+                ++n_p[t];
+                if (t == n_tiles - 1) { umma_commit(&v_empty[j % C::VS]); n_v = j + 1; }
+                return true;
+            };
+            for (int t = 0; ok && t < n_tiles; ++t) ok = scores(0, t, t);
             for (int j = 0; ok && j < n_kb; ++j) {
-                if (j + 1 < n_kb) ok = issue_scores(j + 1);
-                if (!ok) break;
-                const uint32_t v_addr = smem_u32(kv_sm + (size_t)(j % C::STAGES) * C::STAGE + C::K_BYTES);
-#pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    if (t >= n_tiles) break;
-                    if (!wait_or_err(&p_full[t], j & 1, &s_err)) { if (!s_err) s_err = 5; ok = false; break; }
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = umma_desc(p_addr + t * BQ * 128);
-#pragma unroll
-                    for (int kk = 0; kk < 4; ++kk)
-                        umma_bf16(tmem_base + C::O_COL + (uint32_t)(t * HD), da + 2 * kk, umma_desc_sw32(v_addr + kk * HD * 32), idesc_o, (j | kk) != 0);
-                    umma_commit(&o_done[t]);         // the output holds blocks 0..j; the probabilities may be overwritten
+                if (TILES == 1) {
+                    if (j + 1 < n_kb) ok = scores(j + 1, 0, (j + 1) & 1);
+                    if (ok) ok = products(j, 0, j & 1);
+                } else {
+                    for (int t = 0; ok && t < n_tiles; ++t) {
+                        ok = products(j, t, t);
+                        if (ok && j + 1 < n_kb) ok = scores(j + 1, t, t);
+                    }
                 }
-                if (!ok) break;
-                umma_commit(&kv_empty[j % C::STAGES]);
-                n_o = j + 1;
             }
             if (s_err) {
-                for (int t = 0; t < TILES; ++t) drain(s_full[t], 2, n_s[t] & 1, (uint32_t)(n_s[t] >> 1) & 1);
-                drain(kv_empty, C::STAGES, n_o % C::STAGES, (uint32_t)(n_o / C::STAGES) & 1);
-                for (int t = 0; t < TILES; ++t) drain(&o_done[t], 1, 0, (uint32_t)n_o & 1);
+                for (int i = 0; i < 2; ++i)
+                    if (n_s[i]) drain(&s_full[i], 1, 0, (uint32_t)n_s[i] & 1);
+                for (int t = 0; t < TILES; ++t)
+                    if (n_p[t]) drain(&o_done[t], 1, 0, (uint32_t)n_p[t] & 1);
+                drain(k_empty, C::KS, n_k % C::KS, (uint32_t)(n_k / C::KS) & 1);
+                drain(v_empty, C::VS, n_v % C::VS, (uint32_t)(n_v / C::VS) & 1);
             }
         }
     } else {
@@ -262,7 +302,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             if (lane == 0) mbar_arrive(&q_full);
             // does the table name pages that are none?  (then every block's ids are looked at again)
             bool bad = false;
-            for (int p = 4 * kb0 + trow; p < min(n_pages, 4 * (kb0 + n_kb)); p += nq * 32) bad |= !a.kv.holds(s.pt[p]);
+            for (int p = PAGES * kb0 + trow; p < min(n_pages, PAGES * (kb0 + n_kb)); p += nq * 32) bad |= !a.kv.holds(s.pt[p]);
             if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad_page = 1;
             // barriers among softmax warps, bounded like every wait
             auto meet = [&](uint64_t *bar, uint32_t parity) -> bool {
@@ -272,47 +312,49 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             };
             uint32_t tile_phase = 0;
             bool ok = meet(&all_bar, 0);
-            if (!ok && !s_err) s_err = 10;
+            if (!ok && !s_err) s_err = 7;
             const bool bad_pages = s_bad_page != 0;
 
             const uint32_t lane_addr = tmem_base + ((uint32_t)(q * 32) << 16);
             const uint32_t o_addr = lane_addr + C::O_COL + (uint32_t)(t * HD);
-            unsigned char *prow = p_sm + t * BQ * 128 + trow * 128;
             float m_ref = -INFINITY, l = 0.f;
             for (int j = 0; ok && j < n_kb; ++j) {
-                const int buf = j & 1, key0 = (kb0 + j) * BKEY;
-                if (!wait_or_err(&s_full[t][buf], (j >> 1) & 1, &s_err)) { if (!s_err) s_err = 6; ok = false; break; }
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                uint32_t r0[32], r1[32];
-                tmem_ld32(lane_addr + (uint32_t)((t * 2 + buf) * BKEY), r0);
-                tmem_ld32(lane_addr + (uint32_t)((t * 2 + buf) * BKEY + 32), r1);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&s_empty[t][buf]);
-                float sv[64], mx = -INFINITY;
+                const int buf = TILES == 2 ? t : j & 1, key0 = (kb0 + j) * BKEY;
+                const uint32_t s_addr = lane_addr + (uint32_t)(buf * BKEY);
+                const bool tail = key0 + BKEY > s.len, masked = tail || bad_pages;
+                uint64_t vm[2] = {~0ull, ~0ull};
+                if (masked) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    sv[e] = __uint_as_float(r0[e]) * a.scale;
-                    sv[32 + e] = __uint_as_float(r1[e]) * a.scale;
-                }
-                const bool tail = key0 + BKEY > s.len;
-                if (tail || bad_pages) {
-                    uint64_t vm = visible(bits, key0, s.len, s.n_keys);
-                    if (bad_pages)
-                        for (int pg = 0; pg < 4; ++pg) {
-                            const int pi = (key0 >> 4) + pg;
-                            if (pi >= n_pages || !a.kv.holds(s.pt[pi])) vm &= ~(0xffffull << (16 * pg));
+                    for (int h = 0; h < 2; ++h) {
+                        vm[h] = visible(bits, key0 + 64 * h, s.len, s.n_keys);
+                        for (int pg = 0; bad_pages && pg < 4; ++pg) {
+                            const int pi = (key0 >> 4) + 4 * h + pg;
+                            if (pi >= n_pages || !a.kv.holds(s.pt[pi])) vm[h] &= ~(0xffffull << (16 * pg));
                         }
-                    const uint32_t v0 = (uint32_t)vm, v1 = (uint32_t)(vm >> 32);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (!((v0 >> e) & 1)) sv[e] = -INFINITY;
-                        if (!((v1 >> e) & 1)) sv[32 + e] = -INFINITY;
                     }
                 }
+                if (!wait_or_err(&s_full[buf], (TILES == 2 ? j : j >> 1) & 1, &s_err)) { if (!s_err) s_err = 8; ok = false; break; }
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                uint32_t r[2][32];
+                auto mask_chunk = [&](uint32_t (&x)[32], int c) {
+                    const uint32_t v = (uint32_t)(vm[c >> 1] >> (32 * (c & 1)));
 #pragma unroll
-                for (int e = 0; e < 64; ++e) mx = fmaxf(mx, sv[e]);
+                    for (int e = 0; e < 32; ++e)
+                        if (!((v >> e) & 1)) x[e] = 0xff800000u;
+                };
+                // first sweep: the maximum
+                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                tmem_ld32(s_addr, r[0]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    tmem_ld_wait();
+                    if (c < 3) tmem_ld32(s_addr + 32 * (c + 1), r[(c + 1) & 1]);
+                    else tmem_ld32(s_addr, r[0]);                 // (the second sweep's first)
+                    if (masked) mask_chunk(r[c & 1], c);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[c & 1][e]));
+                }
+                const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale;
                 // reference maximum: raised only when the row maximum has outgrown it by RESCALE_STEP
                 float alpha = 1.f;
                 if (m_ref == -INFINITY) {
@@ -323,40 +365,51 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     l *= alpha;
                 }
                 const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-                float psum = 0.f;
+                // second sweep: probabilities, as bf16 over the scores that have been read
+                float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 64; ++e) { sv[e] = ex2f(sv[e] - m_use); psum += sv[e]; }
-                l += psum;
-                // the previous block's P*V has read the probabilities and updated the output
-                if (j > 0 && !wait_or_err(&o_done[t], (j - 1) & 1, &s_err)) { if (!s_err) s_err = 7; ok = false; break; }
+                for (int c = 0; c < 4; ++c) {
+                    tmem_ld_wait();
+                    uint32_t (&x)[32] = r[c & 1];
+                    if (c < 3) tmem_ld32(s_addr + 32 * (c + 1), r[(c + 1) & 1]);
+                    if (masked) mask_chunk(x, c);
+                    float f[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(x[e]);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) fma2(f[e], f[e + 1], a.scale, -m_use);
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        f[e] = ex2f(f[e]); f[e + 1] = ex2f(f[e + 1]); f[e + 2] = ex2f(f[e + 2]); f[e + 3] = ex2f(f[e + 3]);
+                        add2(ps[0], ps[1], f[e], f[e + 1]);
+                        add2(ps[2], ps[3], f[e + 2], f[e + 3]);
+                        pk[e / 2] = pack_bf16(f[e], f[e + 1]);
+                        pk[e / 2 + 1] = pack_bf16(f[e + 2], f[e + 3]);
+                    }
+                    tmem_st16(s_addr + 16 * c, pk);
+                }
+                l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
                 if (__any_sync(0xffffffffu, alpha != 1.f)) {
+                    // (the previous block's products are part of the output; with one tile they may still be running)
+                    if (TILES == 1 && !wait_or_err(&o_done[t], (j - 1) & 1, &s_err)) { if (!s_err) s_err = 9; ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     for (int c0 = 0; c0 < HD; c0 += 32) {
                         uint32_t o[32];
                         tmem_ld32(o_addr + (uint32_t)c0, o);
-                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        tmem_ld_wait();
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
                         tmem_st32(o_addr + (uint32_t)c0, o);
                     }
-                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                }
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    uint4 v;
-                    v.x = pack_bf16(sv[8 * c + 0], sv[8 * c + 1]);
-                    v.y = pack_bf16(sv[8 * c + 2], sv[8 * c + 3]);
-                    v.z = pack_bf16(sv[8 * c + 4], sv[8 * c + 5]);
-                    v.w = pack_bf16(sv[8 * c + 6], sv[8 * c + 7]);
-                    *reinterpret_cast<uint4 *>(prow + ((c ^ (trow & 7)) << 4)) = v;
                 }
                 if (tail && t == 0) {
                     // Values of drafted and of never written slots must not meet a probability of zero as infinity or NaN.  The
                     // first tile's warps look; what they find they zero, by whole tokens, and remember the drafted ones.
-                    unsigned char *vst = kv_sm + (size_t)(j % C::STAGES) * C::STAGE + C::K_BYTES;
-                    if (!wait_or_err(&kv_full[j % C::STAGES], (j / C::STAGES) & 1, &s_err)) { if (!s_err) s_err = 8; ok = false; break; }
+                    unsigned char *vst = v_sm + (j % C::VS) * C::V_BYTES;
+                    if (!wait_or_err(&v_full[j % C::VS], (j / C::VS) & 1, &s_err)) { if (!s_err) s_err = 10; ok = false; break; }
                     bool odd = false;
-                    for (int u = trow; u < 4 * HD * 2; u += nq * 32) {
+                    for (int u = trow; u < PAGES * HD * 2; u += nq * 32) {
                         const uint4 v = *reinterpret_cast<const uint4 *>(vst + u * 16);
                         odd |= odd_pair(v.x) | odd_pair(v.y) | odd_pair(v.z) | odd_pair(v.w);
                     }
@@ -374,26 +427,27 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                         for (int d = lane; d < HD; d += 32) *reinterpret_cast<uint16_t *>(col + d * 32 + (((tk >> 3) ^ ((d >> 2) & 1)) << 4)) = 0;
                         if (lane == 0 && key0 + e < s.n_keys) atomicOr(&s_odd_tokens, 1ull << (key0 + e - s.len));
                     }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // visible to the tensor core's reads
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // visible to the tensor core's reads
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[t]);
+                if (lane == 0) mbar_arrive(&p_full[buf]);
             }
-            if (ok && n_kb > 0 && !wait_or_err(&o_done[t], (n_kb - 1) & 1, &s_err)) { if (!s_err) s_err = 9; ok = false; }
-            if (!meet(&all_bar, 1)) { if (!s_err) s_err = 12; ok = false; }       // both tiles are done with the stages, s_odd_tokens is complete
+            if (ok && n_kb > 0 && !wait_or_err(&o_done[t], (n_kb - 1) & 1, &s_err)) { if (!s_err) s_err = 12; ok = false; }
+            if (!meet(&all_bar, 1)) { if (!s_err) s_err = 13; ok = false; }       // both tiles are done with the rings, s_odd_tokens is complete
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint64_t odd_seen = s_odd_tokens & bits;
             const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
             const size_t head = ((size_t)(a.layer - 1) * a.kv.nkv + kvh) * a.kv.head_elems();
             const float inv = l == 0.f ? 0.f : 1.f / l;            // (l = 0: nothing is visible, the result is zero)
             const size_t out = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD;
-            if (n_splits > 1) *part_ml(p_sm, t * BQ + trow) = make_float2(m_ref, l);
-            float *po = reinterpret_cast<float *>(kv_sm) + (size_t)(t * BQ + trow) * HD;
+            if (n_splits > 1) *part_ml(q_sm, t * BQ + trow) = make_float2(m_ref, l);
+            float *po = reinterpret_cast<float *>(k_sm) + (size_t)(t * BQ + trow) * HD;
             for (int c0 = 0; c0 < HD && n_kb > 0; c0 += 32) {
                 uint32_t o[32];
                 if (ok) tmem_ld32(o_addr + (uint32_t)c0, o);
-                asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                tmem_ld_wait();
                 for (uint64_t left = odd_seen; left; left &= left - 1) {
                     // a drafted token that this row sees and whose values are not finite: added here, in fp32
                     const int pos = s.len + __ffsll((long long)left) - 1;
@@ -421,7 +475,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     }
                 }
             }
-            if (n_splits == 1 && n_kb == 0 && row_ok) {             // a table of no page at all
+            if (n_splits == 1 && n_kb == 0 && row_ok) {             // a table of no position at all
                 for (int e = 0; e < HD; e += 8) {
                     *reinterpret_cast<uint4 *>(a.out + out + e) = make_uint4(0, 0, 0, 0);
                     if (a.out_lo) *reinterpret_cast<uint4 *>(a.out_lo + out + e) = make_uint4(0, 0, 0, 0);
@@ -447,15 +501,15 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
         for (int x = (split * C::THREADS + threadIdx.x) / LPR; x < rows; x += n_splits * C::THREADS / LPR) {
             const int c = threadIdx.x % LPR;
             float M = -INFINITY;
-            for (int k = 0; k < n_splits; ++k) M = fmaxf(M, part_ml(cl.map_shared_rank(p_sm, k), x)->x);
+            for (int k = 0; k < n_splits; ++k) M = fmaxf(M, part_ml(cl.map_shared_rank(q_sm, k), x)->x);
             const float mu = M == -INFINITY ? 0.f : M;
             float L = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int k = 0; k < n_splits; ++k) {
-                const float2 ml = *part_ml(cl.map_shared_rank(p_sm, k), x);
+                const float2 ml = *part_ml(cl.map_shared_rank(q_sm, k), x);
                 if (k * per >= nb) break;                           // (this part and the later ones have no block)
                 const float w = ex2f(ml.x - mu);
-                const float4 v = *reinterpret_cast<const float4 *>(cl.map_shared_rank(reinterpret_cast<float *>(kv_sm), k) + (size_t)x * HD + ((c ^ (x & 15)) << 2));
+                const float4 v = *reinterpret_cast<const float4 *>(cl.map_shared_rank(reinterpret_cast<float *>(k_sm), k) + (size_t)x * HD + ((c ^ (x & 15)) << 2));
                 L += ml.y * w;
                 o.x += v.x * w; o.y += v.y * w; o.z += v.z * w; o.w += v.w * w;
             }
@@ -511,11 +565,11 @@ cudaError_t launch(const Maps &m, const TreeArgs &a, int batch, int max_len, int
     cudaError_t e = attr.set(kern, Cfg<HD, TILES>::SMEM);
     if (e != cudaSuccess) return e;
     const int group = a.nh / a.kv.nkv, n_rt = (a.max_nodes * group + TILES * BQ - 1) / (TILES * BQ);
-    // one CTA per SM: as many parts of the keys as one wave holds, of at least two blocks each
+    // one CTA per SM: as many parts of the keys as one wave holds
     const int64_t units = (int64_t)a.kv.nkv * n_rt * batch;
     const int blocks = (max_len + a.max_nodes + BKEY - 1) / BKEY;
     int splits = (int)(n_sms / units < 8 ? n_sms / units : 8);
-    if (splits > blocks / 2) splits = blocks / 2;
+    if (splits > blocks) splits = blocks;
     if (splits < 1) splits = 1;
     return launch_cluster(kern, dim3(splits, a.kv.nkv * n_rt, batch), Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, splits, st, m, a);
 }
