@@ -1,14 +1,15 @@
 // Beam search's selection (del_beam_select): log softmax, scores and the k best of beams x vocabulary in one pass over the logits.
 //
-// One cluster of CTAs works on one batch item; CTA r owns the same slice of columns of every beam.  Within a beam the score rises
-// with the logit, so each CTA keeps, per beam, the k largest logits of its slice (equal ones: the lower token) beside the running
-// maximum and sum of exponentials.  Then the CTAs share out the beams: the slices' lists are merged, the log-sum-exp turns logits
-// into scores (64 bits: near candidates of different beams are ordered by it); CTA 0 merges the beams' lists.
+// One cluster of CTAs works on one batch item, a CTA on a slice of one beam's row (or on whole rows in turn, with more beams than
+// CTAs).  Within a beam the score rises with the logit, so a CTA keeps the k largest logits of its slice (equal ones: the lower
+// token) beside the running maximum and sum of exponentials.  The slices' lists of a beam are then merged, the log-sum-exp turns
+// logits into scores (64 bits: near candidates of different beams are ordered by it), and CTA 0 merges the beams' lists.
 //
-// The k largest of a block of CHUNK logits, which lie in registers: every warp takes the r-th largest of its threads' maxima,
-// r = ceil(k / warps); the smallest of these over the warps has at least k logits at or above it and, for logits in no special
-// order, few more.  Those are appended to a list and ranked by counting.  Where the list would overflow (sorted logits, say), the
-// k largest are taken one by one instead.
+// The k largest of a slice that streams through registers in chunks of 8192: of the first chunk every warp takes the r-th largest of
+// its threads' maxima, r = ceil(k / warps); the smallest of these over the warps has at least k logits at or above it and, for
+// logits in no special order, few more.  Those go to a list, ranked by counting; the k-th of them is the bar for the next chunks,
+// where hardly any logit passes it.  Where the list would overflow (rising logits, say) the chunk's k largest are taken one by one.
+// What is left per logit is its load, a maximum, a multiply-add, an exponential and a sum.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cstring>
@@ -27,7 +28,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 struct BeamArgs {
     del_beam b;
-    int32_t slice;                         // columns per CTA, a multiple of 8
+    int32_t slices, slice;                 // CTAs per row, columns per CTA (a multiple of 8)
     int32_t aligned;                       // rows start on 16-byte boundaries
 };
 
@@ -61,170 +62,236 @@ struct Shared {
     u64 warp_key[NW];
     float warp_m[NW];
     double warp_s[NW];
-    int count;
-    float m[MAX_BEAMS];                    // per beam: maximum and sum of exponentials of this CTA's slice
+    int count[3];                          // logits listed of chunk i: count[i % 3] (cleared while no thread can still read it)
+    float m[MAX_BEAMS];                    // per row of this CTA: maximum and sum of exponentials of its slice
     double s[MAX_BEAMS];
-    double fin_score[MAX_BEAMS * MAX_K];   // rank 0: the beams' merged lists
+    double fin_score[MAX_BEAMS * MAX_K];   // CTA 0: the beams' merged lists
     int32_t fin_token[MAX_BEAMS * MAX_K];
-    u64 cand[MAX_BEAMS * MAX_K];           // per beam: this CTA's k largest, descending, 0 behind the last
+    u64 cand[MAX_BEAMS * MAX_K];           // per row: its k largest, descending, 0 behind the last
     u64 gather[MAX_CLUSTER * MAX_K];
 };
 
 // the column of element e of this thread in a chunk: vectors of VEC elements, threads side by side
 template <int VEC> __device__ __forceinline__ int column(int e) { return ((e / VEC) * THREADS + threadIdx.x) * VEC + e % VEC; }
 
+__device__ __forceinline__ float ex2f(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// elements [c0, c0 + n) of a row into registers; -inf behind the end
 template <typename T>
-__global__ void __launch_bounds__(THREADS) beam_kernel(const BeamArgs a) {
+__device__ __forceinline__ void load_chunk(float (&x)[EPT], const T *p, int n, bool aligned) {
     constexpr int VEC = 16 / sizeof(T);
+    if (aligned) {
+#pragma unroll
+        for (int v = 0; v < EPT / VEC; ++v) {
+            const int c = column<VEC>(v * VEC);
+            if (c + VEC <= n) {
+                const uint4 q = ldg_stream16(p + c);
+                T t[VEC];
+                memcpy(t, &q, 16);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[v * VEC + e] = to_f<T>(t[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) x[v * VEC + e] = c + e < n ? to_f<T>(p[c + e]) : -INFINITY;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) x[e] = column<VEC>(e) < n ? to_f<T>(p[column<VEC>(e)]) : -INFINITY;
+    }
+}
+
+// The list's k largest, descending, to list[0 .. k) (0 behind the last); returns how many it has.  All threads call.
+__device__ __forceinline__ int prune(Shared &sm, int count, int k) {
+    u64 mine[(LIST + MAX_K + THREADS - 1) / THREADS];
+    int at[(LIST + MAX_K + THREADS - 1) / THREADS];
+#pragma unroll
+    for (int r = 0; r < (LIST + MAX_K + THREADS - 1) / THREADS; ++r) {
+        const int i = threadIdx.x + r * THREADS;
+        at[r] = k;
+        if (i < count) {
+            mine[r] = sm.list[i];
+            int above = 0;
+#pragma unroll 8
+            for (int j = 0; j < count; ++j) above += sm.list[j] > mine[r];
+            at[r] = above;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < (LIST + MAX_K + THREADS - 1) / THREADS; ++r)
+        if (at[r] < k) sm.list[at[r]] = mine[r];
+    for (int i = count + threadIdx.x; i < k; i += THREADS) sm.list[i] = 0;
+    __syncthreads();
+    return min(count, k);
+}
+
+// k largest keys and (maximum, sum of exponentials) of columns [lo, hi) of a row -> cand, m, s of this CTA's row `local`
+template <typename T>
+__device__ void slice_best(Shared &sm, const T *row, int lo, int hi, int k, bool aligned, int local) {
+    constexpr int VEC = 16 / sizeof(T);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float m = -INFINITY, s = 0.f;
+    u64 bar = 0;                                                  // only keys at or above it count
+    float bar_x = -INFINITY;
+    int count = 0;                                                // entries of the list (the same in every thread)
+    float nx[EPT];
+    load_chunk<T>(nx, row + lo, min(CHUNK, hi - lo), aligned);
+    int ci = 0;                                                   // chunk number modulo 3
+    for (int c0 = lo; c0 < hi; c0 += CHUNK, ci = ci == 2 ? 0 : ci + 1) {
+        const int n = min(CHUNK, hi - c0);
+        float x[EPT];
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) x[e] = nx[e];
+        if (c0 + CHUNK < hi) load_chunk<T>(nx, row + c0 + CHUNK, min(CHUNK, hi - c0 - CHUNK), aligned);
+        float cm = x[0];
+#pragma unroll
+        for (int e = 1; e < EPT; ++e) cm = fmaxf(cm, x[e]);
+        // (x - m before the factor: far from zero, the product x * log2 e has lost what the difference needs)
+        const float m_new = fmaxf(m, cm), base = m_new == -INFINITY ? 0.f : m_new;
+        if (m != -INFINITY) s *= ex2f((m - base) * LOG2E);
+        m = m_new;
+        float p0 = 0.f, p1 = 0.f;
+#pragma unroll
+        for (int e = 0; e < EPT; e += 2) {
+            p0 += ex2f((x[e] - base) * LOG2E);
+            p1 += ex2f((x[e + 1] - base) * LOG2E);
+        }
+        s += p0 + p1;
+        if (c0 == lo) {
+            // the bar of the first chunk, from the warps whose threads all have logits
+            const int n_full = min(NW, n / (32 * VEC)), r_th = n_full ? (k + n_full - 1) / n_full : 0;
+            u64 best = 0;
+#pragma unroll
+            for (int e = 0; e < EPT; ++e)
+                if (column<VEC>(e) < n && (best == 0 || x[e] > key_value(best))) best = make_key(x[e], c0 + column<VEC>(e));
+            u64 w = 0;
+            for (int r = 0; r < r_th; ++r) {
+                w = warp_max_u64(best);
+                if (best == w) best = 0;
+            }
+            if (lane == 0) sm.warp_key[warp] = w;
+            if (threadIdx.x < 3) sm.count[threadIdx.x] = 0;
+            __syncthreads();
+            if (n_full && r_th <= 32) {                           // (r_th > 32: fewer than 64 threads' logits, all of them are listed)
+                bar = ~0ull;
+                for (int i = 0; i < n_full; ++i) bar = min(bar, sm.warp_key[i]);
+                bar_x = bar ? key_value(bar) : -INFINITY;
+            }
+        }
+        if (!(cm < bar_x)) {                                      // (a NaN passes on to the key's comparison)
+#pragma unroll
+            for (int e = 0; e < EPT; ++e)
+                if (!(x[e] < bar_x) && column<VEC>(e) < n) {
+                    const u64 key = make_key(x[e], c0 + column<VEC>(e));
+                    if (key >= bar) {
+                        const int at = count + atomicAdd(&sm.count[ci], 1);
+                        if (at < LIST) sm.list[at] = key;
+                    }
+                }
+        }
+        if (threadIdx.x == 0) sm.count[ci == 2 ? 0 : ci + 1] = 0;
+        __syncthreads();
+        int now = count + sm.count[ci];
+        if (now > LIST) {
+            // too many: the chunk's k largest one by one, behind what was there
+            u64 last = ~0ull;
+            now = count;
+            for (int i = 0; i < k; ++i) {
+                u64 next = 0;
+#pragma unroll
+                for (int e = 0; e < EPT; ++e)
+                    if (column<VEC>(e) < n) {
+                        const u64 key = make_key(x[e], c0 + column<VEC>(e));
+                        if (key < last && key > next) next = key;
+                    }
+                next = warp_max_u64(next);
+                __syncthreads();
+                if (lane == 0) sm.warp_key[warp] = next;
+                __syncthreads();
+                for (int j = 0; j < NW; ++j) next = max(next, sm.warp_key[j]);
+                if (next == 0) break;
+                if (threadIdx.x == 0) sm.list[now] = next;
+                last = next;
+                ++now;
+            }
+            __syncthreads();
+        }
+        count = now;
+        if (c0 + CHUNK >= hi || c0 == lo || count > LIST / 4) {
+            count = prune(sm, count, k);
+            if (count == k) {
+                bar = sm.list[k - 1];
+                bar_x = key_value(bar);
+            }
+        }
+    }
+    // sums of the threads, in double
+    float wm = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
+    double ws = m == -INFINITY ? (double)s : (double)(s * ex2f((m - wm) * LOG2E));       // (m = -inf: 0, or no number)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+    if (lane == 0) { sm.warp_m[warp] = wm; sm.warp_s[warp] = ws; }
+    for (int i = threadIdx.x; i < k; i += THREADS) sm.cand[local * k + i] = i < count ? sm.list[i] : 0;
+    __syncthreads();
+    if (warp == 0) {
+        const float tm = lane < NW ? sm.warp_m[lane] : -INFINITY;
+        const double ts = lane < NW ? sm.warp_s[lane] : 0.0;
+        float M = tm;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+        double S = tm == -INFINITY ? ts : ts * (double)ex2f((tm - M) * LOG2E);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+        if (lane == 0) { sm.m[local] = M; sm.s[local] = S; }
+    }
+    __syncthreads();
+}
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS, 2) beam_kernel(const BeamArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     Shared &sm = *reinterpret_cast<Shared *>(smem);
     cg::cluster_group cl = cg::this_cluster();
     const int rank = cl.block_rank(), n_ranks = cl.num_blocks();
-    const int item = blockIdx.x / n_ranks, beams = a.b.beams, V = a.b.vocab, k = a.b.k;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int lo = min((int64_t)rank * a.slice, (int64_t)V), hi = min((int64_t)lo + a.slice, (int64_t)V);
-
-    for (int e = threadIdx.x; e < beams * k; e += THREADS) sm.cand[e] = 0;
-    for (int e = threadIdx.x; e < beams; e += THREADS) { sm.m[e] = -INFINITY; sm.s[e] = 0.0; }
-    __syncthreads();
-    for (int beam = 0; beam < beams; ++beam) {
+    const int item = blockIdx.x / n_ranks, beams = a.b.beams, V = a.b.vocab, k = a.b.k, slices = a.slices;
+    // rank = beam * slices + slice; with more beams than CTAs (slices = 1) beams rank, rank + n_ranks, ...
+    for (int e = threadIdx.x; e < MAX_BEAMS; e += THREADS) { sm.m[e] = -INFINITY; sm.s[e] = 0.0; }
+    const int lo = (int)min((int64_t)(rank % slices) * a.slice, (int64_t)V), hi = (int)min((int64_t)lo + a.slice, (int64_t)V);
+    int local = 0;
+    for (int beam = rank / slices; beam < beams; beam += n_ranks, ++local) {
         const int row = item * beams + beam;
         if (a.b.finished && a.b.finished[row]) continue;
-        const T *logits = reinterpret_cast<const T *>(a.b.logits) + row * a.b.row_stride;
-        for (int c0 = lo; c0 < hi; c0 += CHUNK) {
-            const int n = min(CHUNK, hi - c0);
-            float x[EPT];
-            if (a.aligned) {
-#pragma unroll
-                for (int v = 0; v < EPT / VEC; ++v) {
-                    const int c = column<VEC>(v * VEC);
-                    if (c + VEC <= n) {
-                        const uint4 q = ldg_stream16(logits + c0 + c);
-                        T t[VEC];
-                        memcpy(t, &q, 16);
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) x[v * VEC + e] = to_f<T>(t[e]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) x[v * VEC + e] = c + e < n ? to_f<T>(logits[c0 + c + e]) : -INFINITY;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < EPT; ++e) x[e] = column<VEC>(e) < n ? to_f<T>(logits[c0 + column<VEC>(e)]) : -INFINITY;
-            }
-            // maximum, sum of exponentials, this thread's best key
-            float m = -INFINITY;
-            u64 best = 0;
-#pragma unroll
-            for (int e = 0; e < EPT; ++e) {
-                m = fmaxf(m, x[e]);
-                if (column<VEC>(e) < n) {
-                    const u64 key = make_key(x[e], c0 + column<VEC>(e));
-                    if (key > best) best = key;
-                }
-            }
-            const float base = m == -INFINITY ? 0.f : m;
-            float s = 0.f;
-#pragma unroll
-            for (int e = 0; e < EPT; ++e) s += exp2f((x[e] - base) * LOG2E);
-            float wm = m;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-            double ws = m == -INFINITY ? (double)s : (double)s * (double)exp2f((m - wm) * LOG2E);      // (m = -inf: 0, or no number)
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
-            // the r-th largest thread maximum of the warp, of those warps whose threads all have logits
-            const int n_full = min(NW, n / (32 * VEC));
-            const int r_th = n_full ? (k + n_full - 1) / n_full : 0;
-            u64 mine = best, w = 0;
-            for (int r = 0; r < r_th; ++r) {
-                w = warp_max_u64(mine);
-                if (mine == w) mine = 0;
-            }
-            if (lane == 0) { sm.warp_key[warp] = w; sm.warp_m[warp] = wm; sm.warp_s[warp] = ws; }
-            if (threadIdx.x == 0) sm.count = 0;
-            __syncthreads();
-            u64 least = 0;                                        // (r_th > 32: fewer than 64 threads' logits, all of them are listed)
-            if (n_full && r_th <= 32) {
-                least = ~0ull;
-                for (int i = 0; i < n_full; ++i) least = min(least, sm.warp_key[i]);
-            }
-            const u64 kth = sm.cand[beam * k + k - 1];
-            if (kth > least) least = kth;
-#pragma unroll
-            for (int e = 0; e < EPT; ++e)
-                if (column<VEC>(e) < n) {
-                    const u64 key = make_key(x[e], c0 + column<VEC>(e));
-                    if (key >= least) {
-                        const int at = atomicAdd(&sm.count, 1);
-                        if (at < LIST) sm.list[at] = key;
-                    }
-                }
-            __syncthreads();
-            int count = sm.count;
-            if (count > LIST) {                                   // (the same in every thread)
-                u64 last = ~0ull;
-                count = 0;
-                for (int i = 0; i < k; ++i) {
-                    u64 next = 0;
-#pragma unroll
-                    for (int e = 0; e < EPT; ++e)
-                        if (column<VEC>(e) < n) {
-                            const u64 key = make_key(x[e], c0 + column<VEC>(e));
-                            if (key < last && key > next) next = key;
-                        }
-                    next = warp_max_u64(next);
-                    __syncthreads();
-                    if (lane == 0) sm.warp_key[warp] = next;
-                    __syncthreads();
-                    for (int j = 0; j < NW; ++j) next = max(next, sm.warp_key[j]);
-                    if (next == 0) break;
-                    if (threadIdx.x == 0) sm.list[i] = next;
-                    last = next;
-                    ++count;
-                }
-                __syncthreads();
-            }
-            // with what the beam had already; ranked by counting
-            for (int i = threadIdx.x; i < k; i += THREADS) sm.list[count + i] = sm.cand[beam * k + i];
-            if (threadIdx.x == 0) {
-                float M = sm.m[beam];
-                for (int i = 0; i < NW; ++i) M = fmaxf(M, sm.warp_m[i]);
-                const float b0 = M == -INFINITY ? 0.f : M;
-                double S = sm.m[beam] == -INFINITY ? sm.s[beam] : sm.s[beam] * (double)exp2f((sm.m[beam] - b0) * LOG2E);
-                for (int i = 0; i < NW; ++i) S += sm.warp_m[i] == -INFINITY ? sm.warp_s[i] : sm.warp_s[i] * (double)exp2f((sm.warp_m[i] - b0) * LOG2E);
-                sm.m[beam] = M;
-                sm.s[beam] = S;
-            }
-            __syncthreads();
-            const int total = count + k;
-            for (int i = threadIdx.x; i < total; i += THREADS) {
-                const u64 key = sm.list[i];
-                if (key == 0) continue;
-                int above = 0;
-                for (int j = 0; j < total; ++j) above += sm.list[j] > key;
-                if (above < k) sm.cand[beam * k + above] = key;
-            }
-            __syncthreads();
-        }
+        if (lo < hi) slice_best<T>(sm, reinterpret_cast<const T *>(a.b.logits) + row * a.b.row_stride, lo, hi, k, a.aligned, local);
+        else
+            for (int i = threadIdx.x; i < k; i += THREADS) sm.cand[local * k + i] = 0;
     }
     cl.sync();
-    // beams shared out: the slices' lists become one list of scores in CTA 0
+    // each beam's first CTA: the slices' lists become one list of scores in CTA 0
     double *fin_score = cl.map_shared_rank(sm.fin_score, 0);
     int32_t *fin_token = cl.map_shared_rank(sm.fin_token, 0);
-    for (int beam = rank; beam < beams; beam += n_ranks) {
+    local = 0;
+    for (int beam = rank / slices; beam < beams && rank % slices == 0; beam += n_ranks, ++local) {
         const int row = item * beams + beam;
         const double cum = a.b.scores[row];
         const bool done = a.b.finished && a.b.finished[row];
-        float M = -INFINITY;
-        for (int r = 0; r < n_ranks; ++r) M = fmaxf(M, cl.map_shared_rank(sm.m, r)[beam]);
-        double S = 0.0;
-        for (int r = 0; r < n_ranks; ++r) {
-            const float m = cl.map_shared_rank(sm.m, r)[beam];
-            S += cl.map_shared_rank(sm.s, r)[beam] * (m == -INFINITY ? 1.0 : exp((double)m - (double)M));
+        double lse = 0.0;
+        if (!done) {
+            float M = -INFINITY;
+            for (int r = 0; r < slices; ++r) M = fmaxf(M, cl.map_shared_rank(sm.m, rank + r)[local]);
+            double S = 0.0;
+            for (int r = 0; r < slices; ++r) {
+                const float m = cl.map_shared_rank(sm.m, rank + r)[local];
+                S += cl.map_shared_rank(sm.s, rank + r)[local] * (m == -INFINITY ? 1.0 : (double)ex2f((m - M) * LOG2E));
+            }
+            lse = (double)M + log(S);
         }
-        const double lse = (double)M + log(S);
         const bool dead = !(cum > -INFINITY && cum < INFINITY) || !(lse > -INFINITY && lse < INFINITY);
         if (done || dead) {
             // one continuation at most; behind it the lowest tokens at -inf
@@ -237,14 +304,19 @@ __global__ void __launch_bounds__(THREADS) beam_kernel(const BeamArgs a) {
             continue;                                             // (the whole CTA)
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < n_ranks * k; e += THREADS) sm.gather[e] = cl.map_shared_rank(sm.cand, e / k)[beam * k + e % k];
+        for (int e = threadIdx.x; e < slices * k; e += THREADS) sm.gather[e] = cl.map_shared_rank(sm.cand, rank + e / k)[local * k + e % k];
         __syncthreads();
-        if (threadIdx.x < k && V < k && (int)threadIdx.x >= V) fin_token[beam * k + threadIdx.x] = -1;       // (a live row lists min(k, V))
-        for (int e = threadIdx.x; e < n_ranks * k; e += THREADS) {
+        if (threadIdx.x < k && (int)threadIdx.x >= V) fin_token[beam * k + threadIdx.x] = -1;       // (a live row lists min(k, V))
+        for (int e = threadIdx.x; e < slices * k; e += THREADS) {
             const u64 key = sm.gather[e];
             if (key == 0) continue;
-            int above = 0;
-            for (int j = 0; j < n_ranks * k; ++j) above += sm.gather[j] > key;
+            int above = e % k;                                    // its place in its own list; the others descend as well
+            for (int r = 0; r < slices && above < k; ++r) {
+                if (r == e / k) continue;
+                int n = 0;
+                while (n < k && sm.gather[r * k + n] > key) ++n;
+                above += n;
+            }
             if (above < k) {
                 fin_score[beam * k + above] = cum + ((double)key_value(key) - lse);
                 fin_token[beam * k + above] = key_token(key);
@@ -308,10 +380,16 @@ extern "C" int del_beam_select(const del_beam *x, void *cuda_stream) {
     memset(&a, 0, sizeof(a));
     a.b = *x;
     a.aligned = ((uintptr_t)x->logits & 15) == 0 && (x->row_stride * size) % 16 == 0;
-    int ranks = 1;
-    while (ranks < MAX_CLUSTER && ranks * 2 * x->batch <= 2 * n_sms && ranks * 1024 < x->vocab) ranks *= 2;
-    a.slice = ((x->vocab + ranks - 1) / ranks + 7) / 8 * 8;
+    // CTAs per item: two per SM over all items, at most 16 (a cluster), none with less than 2048 columns (a smaller slice is all
+    // latency); whole rows per CTA where there are more beams than CTAs
+    int64_t ranks = 2 * (int64_t)n_sms / x->batch, most = (int64_t)x->beams * ((x->vocab + 2047) / 2048);
+    if (ranks > MAX_CLUSTER) ranks = MAX_CLUSTER;
+    if (ranks > most) ranks = most;
+    if (ranks < 1) ranks = 1;
+    a.slices = ranks >= x->beams ? (int)(ranks / x->beams) : 1;
+    if (ranks >= x->beams) ranks = (int64_t)a.slices * x->beams;
+    a.slice = ((x->vocab + a.slices - 1) / a.slices + 7) / 8 * 8;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = x->dtype == DEL_F32 ? launch<float>(a, ranks, st) : x->dtype == DEL_BF16 ? launch<bf16>(a, ranks, st) : launch<__half>(a, ranks, st);
+    const cudaError_t e = x->dtype == DEL_F32 ? launch<float>(a, (int)ranks, st) : x->dtype == DEL_BF16 ? launch<bf16>(a, (int)ranks, st) : launch<__half>(a, (int)ranks, st);
     return e == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }
