@@ -398,7 +398,8 @@ int del_kv_fork(const del_pages *kv, const del_fork_args *args, void *cuda_strea
  * logit, then the lower token id.  finished (may be null): a row with a non-zero entry has one continuation, token eos at its score
  * unchanged.  A score that is no number below +inf counts as -inf (a row whose logits hold a NaN or +inf has only such);
  * continuations at -inf are chosen last.  The order is taken in 64 bits, the log-sum-exp is accurate to fp32.
- * 1 <= k <= 64, 1 <= beams <= 64, k <= beams * vocab, eos in [0, vocab) if finished is given. */
+ * 1 <= k <= 64, 1 <= beams <= 64, batch * beams <= 65535, k <= beams * vocab, eos in [0, vocab) if finished is given.  DEL_ENOSPC:
+ * workspace too small. */
 enum { DEL_F32 = 0, DEL_BF16 = 1, DEL_F16 = 2 };
 typedef struct {
     const void *logits;           /* [batch * beams] rows of vocab values of `dtype`, row_stride elements apart */
@@ -406,9 +407,13 @@ typedef struct {
     const uint8_t *finished;
     float *out_scores;            /* [batch][k] */
     int32_t *out_tokens, *out_rows;          /* [batch][k]; out_rows = item * beams + beam: the parents of del_kv_fork */
+    void *workspace;              /* 16-byte aligned, workspace_bytes >= del_beam_workspace_bytes; its contents are clobbered.  Calls */
+    size_t workspace_bytes;       /* that may overlap on the GPU (other streams, graphs replayed side by side) need one each */
     int64_t row_stride;
     int32_t batch, beams, vocab, k, eos, dtype;
 } del_beam;
+/* Bytes for a call of this shape (batch, beams, vocab, k); host arithmetic only; 0 if the shape is refused. */
+size_t del_beam_workspace_bytes(const del_beam *args);
 int del_beam_select(const del_beam *args, void *cuda_stream);
 
 const char *del_strerror(int code);

@@ -31,7 +31,7 @@ EXPORTS = ["del_workspace_bytes", "del_init", "del_prefill", "del_draft", "del_v
            "del_get_drafts", "del_force_token", "del_get_hidden", "del_debug_logits", "del_get_kv", "del_committed_len", "del_release",
            "del_launch_count", "del_get_traffic", "del_set_flags", "del_get_kernel_times", "del_head_argmax_static",
            "del_set_policy_fs", "del_set_exit_mode", "del_get_window", "del_set_sampling", "del_get_sample_info", "del_get_round_logits", "del_sample_probe", "del_get_conf_stats", "del_set_conf_stats", "del_get_conf", "del_debug_inject_error", "del_debug_routes",
-           "del_tree_attention", "del_kv_compact", "del_kv_fork", "del_beam_select", "del_strerror", "del_last_cuda_error", "del_destroy"]
+           "del_tree_attention", "del_kv_compact", "del_kv_fork", "del_beam_select", "del_beam_workspace_bytes", "del_strerror", "del_last_cuda_error", "del_destroy"]
 
 
 class Shape(C.Structure):
@@ -86,8 +86,8 @@ class ForkC(C.Structure):
 
 
 class BeamC(C.Structure):
-    _fields_ = [(n, C.c_void_p) for n in ("logits", "scores", "finished", "out_scores", "out_tokens", "out_rows")] + \
-               [("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("batch", "beams", "vocab", "k", "eos", "dtype")]
+    _fields_ = [(n, C.c_void_p) for n in ("logits", "scores", "finished", "out_scores", "out_tokens", "out_rows", "workspace")] + \
+               [("workspace_bytes", C.c_size_t), ("row_stride", C.c_int64)] + [(n, C.c_int32) for n in ("batch", "beams", "vocab", "k", "eos", "dtype")]
 
 
 _lib = None
@@ -182,6 +182,8 @@ def load_library(build_if_missing: bool = True):
         getattr(L, name).argtypes = [vp, vp, vp]
     L.del_beam_select.restype = ci
     L.del_beam_select.argtypes = [vp, vp]
+    L.del_beam_workspace_bytes.restype = C.c_size_t
+    L.del_beam_workspace_bytes.argtypes = [vp]
     L.del_strerror.restype = C.c_char_p
     L.del_strerror.argtypes = [ci]
     L.del_last_cuda_error.restype = C.c_char_p
@@ -486,7 +488,7 @@ def head_argmax_static(x, lm_head, tokens_out, stream=None) -> int:
 # These calls are a few microseconds of GPU work in a loop over layers or steps: the checks below look at each tensor once, and
 # the C structs are packed as bytes (a ctypes structure of 24 fields takes 3 us to fill, packed bytes 1 us).
 _PACK_PAGES, _PACK_TREE = _struct.Struct("=2Q4i").pack, _struct.Struct("=8Q4q7if").pack
-_PACK_COMPACT, _PACK_FORK, _PACK_BEAM = _struct.Struct("=5Q7i4x").pack, _struct.Struct("=9Q8i").pack, _struct.Struct("=6Qq6i").pack
+_PACK_COMPACT, _PACK_FORK, _PACK_BEAM = _struct.Struct("=5Q7i4x").pack, _struct.Struct("=9Q8i").pack, _struct.Struct("=8Qq6i").pack
 
 
 def _refuse(what: str, why: str):
@@ -613,11 +615,12 @@ def kv_fork(k_pages, v_pages, table, lens, parents, spare, n_spare, new_table, n
     _call(what, dev, load_library().del_kv_fork, kv, a, stream)
 
 
-def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None, eos: int = 0, stream=None):
+def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None, eos: int = 0, workspace=None, stream=None):
     """del_beam_select: the k best continuations of every item, k = out_scores.shape[1].
 
     logits fp32, bf16 or fp16 [batch, beams, vocab] (equally spaced rows); scores fp32 [batch, beams]; finished bool [batch, beams];
-    out_scores fp32, out_tokens and out_rows int32 [batch, k].  out_rows = item * beams + beam."""
+    out_scores fp32, out_tokens and out_rows int32 [batch, k].  out_rows = item * beams + beam.  workspace: uint8 tensor of
+    del_beam_workspace_bytes, made for the call when None."""
     global _t
     if _t is None:
         import torch
@@ -644,6 +647,13 @@ def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None,
     for t in (out_tokens, out_rows):
         if t.shape != out or t.dtype is not _t.int32 or t.get_device() != dev or not t.is_contiguous():
             _refuse(what, "out_tokens, out_rows: contiguous int32 [batch, k] on the logits' device expected")
-    a = _PACK_BEAM(logits.data_ptr(), scores.data_ptr(), fp, out_scores.data_ptr(), out_tokens.data_ptr(), out_rows.data_ptr(), row, batch,
-                   beams, vocab, out[1], eos, dtype)
-    _call(what, dev, load_library().del_beam_select, None, a, stream)
+    lib = load_library()
+    head = (logits.data_ptr(), scores.data_ptr(), fp, out_scores.data_ptr(), out_tokens.data_ptr(), out_rows.data_ptr())
+    tail = (row, batch, beams, vocab, out[1], eos, dtype)
+    if workspace is None:
+        workspace = _t.empty(lib.del_beam_workspace_bytes(_PACK_BEAM(*head, 0, 0, *tail)), dtype=_t.uint8, device=logits.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    elif workspace.dtype is not _t.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse(what, "workspace: contiguous uint8 on the logits' device expected")
+    _call(what, dev, lib.del_beam_select, None, _PACK_BEAM(*head, workspace.data_ptr(), workspace.numel(), *tail), stream)

@@ -1,9 +1,11 @@
 // Beam search's selection (del_beam_select): log softmax, scores and the k best of beams x vocabulary in one pass over the logits.
 //
-// One cluster of CTAs works on one batch item, a CTA on a slice of one beam's row (or on whole rows in turn, with more beams than
-// CTAs).  Within a beam the score rises with the logit, so a CTA keeps the k largest logits of its slice (equal ones: the lower
-// token) beside the running maximum and sum of exponentials, and leaves them in the shared memory of the cluster's first CTA.  That
-// one turns logits into scores (64 bits: near candidates of different beams are ordered by them) and merges the lists.
+// A CTA takes a slice of one row.  Within a row the score rises with the logit, so the CTA keeps the k largest logits of its slice
+// (equal ones: the lower token) beside the running maximum and sum of exponentials, and leaves them in the workspace.  One CTA per
+// item then turns the slices' logits into scores (64 bits: near candidates of different rows are ordered by them) and takes the k best.
+// Small calls do both in one launch, an item's CTAs being a cluster; the others in two, the second starting while the first
+// drains.  B200 keeps 15 clusters of 8 or 7 of 16 resident with one CTA per SM: 16 x 8 x 128256 takes 59 us in clusters of 8 (two
+// waves), 25 us as 128 free CTAs, but a second launch costs the host 4 us (1 x 4 x 32000: 10 us a call in one launch, 13 in two).
 //
 // The k largest of a slice that streams through registers in chunks: of the first chunk every warp lists the largest of its threads'
 // maxima, r = k / 4 of them; the k-th of all listed is a bar that at least k logits reach and, for logits in no special order, hardly
@@ -18,26 +20,27 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cstring>
-#include <utility>
 
 #include "pages.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace {
 
 typedef unsigned long long u64;
 
-constexpr int THREADS = 512, NW = THREADS / 32, NV = 2, MAX_K = 64, MAX_BEAMS = 64, MAX_CLUSTER = 16;
+constexpr int THREADS = 512, NW = THREADS / 32, NV = 4, MAX_K = 64, MAX_BEAMS = 64, MAX_CAND = 4096, MAX_CLUSTER = 16;
 constexpr int GROUP = 4;                   // chunks between two looks at the list's length
 constexpr int LIST = 1024;                 // candidates of a slice that are ranked by counting
-constexpr int LISTS = MAX_BEAMS;           // most lists of an item: beams x slices <= MAX_CLUSTER, or one per beam
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct BeamArgs {
     del_beam b;
     int32_t slices, slice;                 // CTAs per row, columns per CTA (a multiple of 8)
     int32_t aligned;                       // rows start on 16-byte boundaries
+    int32_t fused;                         // one launch, an item's CTAs a cluster
+    // workspace: list = row * slices + slice
+    u64 *key;                              // [lists][k], descending, 0 behind the last
+    double *s;                             // [lists] sums of exponentials
+    float *m;                              // [lists] maxima
 };
 
 // Logits in the order of their value as unsigned numbers; the key of a token puts equal logits in the order of their ids.
@@ -71,13 +74,41 @@ struct Shared {
     float warp_m[NW];
     double warp_s[NW];
     int count[3];                          // logits listed of group i: count[i % 3] (cleared while no thread can still read it)
-    // the cluster's first CTA: list i belongs to beam i / slices
-    u64 key[LISTS * MAX_K];                // k each, descending, 0 behind the last
-    float m[LISTS];                        // maximum and sum of exponentials of the slice
-    double s[LISTS];
-    double score[LISTS * MAX_K];
-    double lse[MAX_BEAMS];
 };
+
+// (each function names the array itself: through a pointer the accesses would be generic ones)
+__device__ __forceinline__ Shared &shared() {
+    extern __shared__ __align__(16) unsigned char smem[];
+    return *reinterpret_cast<Shared *>(smem);
+}
+
+// Of one number per thread (0: none): the k-th largest of those listed, r per warp; 0 if fewer are.  At least k of the numbers reach it.
+// All threads call; ends with a barrier.
+__device__ __forceinline__ u64 kth_of_threads(Shared &sm, u64 mine, int k, int r) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t hi = (uint32_t)(mine >> 32), lo = (uint32_t)mine;
+    for (int i = 0; i < r; ++i) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, hi), low = __reduce_max_sync(0xffffffffu, hi == top ? lo : 0u);
+        const uint32_t who = __ballot_sync(0xffffffffu, hi == top && lo == low);
+        if (lane == 0) sm.warp_key[warp * r + i] = ((u64)top << 32) | low;
+        if (lane == __ffs(who) - 1) hi = lo = 0;
+    }
+    if (threadIdx.x == 0) sm.bar = 0;
+    __syncthreads();
+    if ((int)threadIdx.x < NW * r) {
+        const u64 key = sm.warp_key[threadIdx.x];
+        int above = 0, before = 0;                                // equal numbers: in the order of the list
+#pragma unroll 8
+        for (int i = 0; i < NW * r; ++i) {
+            const u64 o = sm.warp_key[i];
+            above += o > key;
+            before += o == key && i < (int)threadIdx.x;
+        }
+        if (key && above + before == k - 1) sm.bar = key;
+    }
+    __syncthreads();
+    return sm.bar;
+}
 
 // a chunk: NV vectors of 16 bytes per thread, threads side by side
 template <typename T> struct Chunk {
@@ -91,25 +122,45 @@ __device__ __forceinline__ float ex2f(float x) {
     return y;
 }
 
-// elements [0, n) of p into registers; what lies behind the end is left as it is
+// two lanes of fp32 arithmetic in one instruction: (x - a) * b, and x += b
+__device__ __forceinline__ void sub_mul2(float &x0, float &x1, float a, float b) {
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+        "add.rn.f32x2 x, x, y;\n\tmul.rn.f32x2 x, x, z;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(x0), "+f"(x1) : "f"(-a), "f"(b));
+}
+__device__ __forceinline__ void add2(float &x0, float &x1, float b0, float b1) {
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "+f"(x0), "+f"(x1) : "f"(b0), "f"(b1));
+}
+
+template <typename T> __device__ __forceinline__ T minus_infinity() { return T(-INFINITY); }
+template <> __device__ __forceinline__ bf16 minus_infinity<bf16>() { return __ushort_as_bfloat16(0xff80); }
+template <> __device__ __forceinline__ __half minus_infinity<__half>() { return __ushort_as_half(0xfc00); }
+
+// elements [0, n) of p into registers, -inf behind the end
 template <typename T>
 __device__ __forceinline__ void load_chunk(uint4 (&q)[NV], const T *p, int n, bool aligned) {
     using C = Chunk<T>;
+    if (aligned && n >= C::SIZE) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int c = C::column(v * C::VEC);
-        if (aligned && c + C::VEC <= n) q[v] = ldg_stream16(p + c);
-        else if (c < n) {
-            T t[C::VEC];
+        for (int v = 0; v < NV; ++v) q[v] = ldg_stream16(p + C::column(v * C::VEC));
+    } else {
 #pragma unroll
-            for (int e = 0; e < C::VEC; ++e) t[e] = p[min(c + e, n - 1)];
-            memcpy(&q[v], t, 16);
+        for (int v = 0; v < NV; ++v) {
+            const int c = C::column(v * C::VEC);
+            if (aligned && c + C::VEC <= n) q[v] = ldg_stream16(p + c);
+            else {
+                T t[C::VEC];
+#pragma unroll
+                for (int e = 0; e < C::VEC; ++e) t[e] = c + e < n ? p[c + e] : minus_infinity<T>();
+                memcpy(&q[v], t, 16);
+            }
         }
     }
 }
 
 // The list's k largest, descending, to list[0 .. k) (0 behind the last); returns how many it has.  All threads call.
-__device__ __noinline__ int prune(Shared &sm, int count, int k) {
+__device__ __noinline__ int prune(int count, int k) {
+    Shared &sm = shared();
     constexpr int N = (LIST + MAX_K + THREADS - 1) / THREADS;
     u64 mine[N];
     int at[N];
@@ -138,7 +189,8 @@ __device__ __noinline__ int prune(Shared &sm, int count, int k) {
 
 // the k largest of p[0, n) one by one, behind the list's first `count` entries; returns the new count.  All threads call.
 template <typename T>
-__device__ __noinline__ int take_largest(Shared &sm, const T *p, int first_token, int n, int count, int k) {
+__device__ __noinline__ int take_largest(const T *p, int first_token, int n, int count, int k) {
+    Shared &sm = shared();
     u64 last = ~0ull;
     for (int i = 0; i < k; ++i) {
         u64 next = 0;
@@ -165,16 +217,16 @@ template <typename T>
 __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int hi, int k, bool aligned, float &m_out, double &s_out) {
     using C = Chunk<T>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float m = -INFINITY, s = 0.f;
+    float m = -INFINITY, s0 = 0.f, s1 = 0.f;
     u64 bar = 0;                                                  // only keys at or above it count
     float bar_x = -INFINITY;
     int count = 0;                                                // entries of the list (the same in every thread)
     int gi = 0;                                                   // group number modulo 3
 
-    auto load = [&](uint4 (&q)[NV], int c0) {
+    auto load = [&](uint4 (&q)[NV], int c0) __attribute__((always_inline)) {
         if (c0 < hi) load_chunk<T>(q, row + c0, min(C::SIZE, hi - c0), aligned);
     };
-    auto work = [&](uint4 (&q)[NV], int c0) {
+    auto work = [&](uint4 (&q)[NV], int c0) __attribute__((always_inline)) {
         const int n = min(C::SIZE, hi - c0);
         float x[C::EPT];
 #pragma unroll
@@ -182,63 +234,53 @@ __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int 
             T t[C::VEC];
             memcpy(t, &q[v], 16);
 #pragma unroll
-            for (int e = 0; e < C::VEC; ++e) x[v * C::VEC + e] = n == C::SIZE || C::column(v * C::VEC + e) < n ? to_f<T>(t[e]) : -INFINITY;
+            for (int e = 0; e < C::VEC; ++e) x[v * C::VEC + e] = to_f<T>(t[e]);
         }
         load(q, c0 + 2 * C::SIZE);
-        float cm = x[0];
+        float c2[2] = {x[0], x[1]};
 #pragma unroll
-        for (int e = 1; e < C::EPT; ++e) cm = fmaxf(cm, x[e]);
+        for (int e = 2; e < C::EPT; ++e) c2[e & 1] = fmaxf(c2[e & 1], x[e]);
+        const float cm = fmaxf(c2[0], c2[1]);
         // (x - m before the factor: far from zero, the product x * log2 e has lost what the difference needs)
-        const float m_new = fmaxf(m, cm), base = m_new == -INFINITY ? 0.f : m_new;
-        if (m != -INFINITY) s *= ex2f((m - base) * LOG2E);
-        m = m_new;
-        float p0 = 0.f, p1 = 0.f;
+        if (cm > m) {
+            const float f = m == -INFINITY ? 1.f : ex2f((m - cm) * LOG2E);      // (before the first number: sums of 0, or no number)
+            s0 *= f;
+            s1 *= f;
+            m = cm;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int e = 0; e < C::EPT; e += 2) {
-            p0 += ex2f((x[e] - base) * LOG2E);
-            p1 += ex2f((x[e + 1] - base) * LOG2E);
+            float d0 = x[e], d1 = x[e + 1];
+            sub_mul2(d0, d1, base, LOG2E);
+            add2(s0, s1, ex2f(d0), ex2f(d1));
         }
-        s += p0 + p1;
         if (c0 == lo) {
             // the first bar, from the warps' lists of their threads' maxima (f: warps whose threads all have logits)
             const int f = min(NW, n / (32 * C::VEC)), r_th = f ? max((k + 3) / 4, (k + f - 1) / f) : 33;
             if (threadIdx.x < 3) sm.count[threadIdx.x] = 0;
-            if (threadIdx.x == 0) sm.bar = 0;
             if (r_th <= 32) {                                     // (else fewer than 64 threads' logits: all of them are listed)
-                uint32_t hi32 = 0, lo32 = 0;
+                u64 best = 0;
                 if (C::column(0) < n) {
                     int at = 0;
 #pragma unroll
                     for (int e = C::EPT - 1; e >= 0; --e)
                         if (x[e] == cm && C::column(e) < n) at = e;
-                    const u64 best = make_key(cm, c0 + C::column(at));
-                    hi32 = (uint32_t)(best >> 32);
-                    lo32 = (uint32_t)best;
+                    best = make_key(cm, c0 + C::column(at));
                 }
-                for (int r = 0; r < r_th; ++r) {
-                    const uint32_t top = __reduce_max_sync(0xffffffffu, hi32), low = __reduce_max_sync(0xffffffffu, hi32 == top ? lo32 : 0u);
-                    if (lane == 0) sm.warp_key[warp * r_th + r] = ((u64)top << 32) | low;
-                    if (hi32 == top && lo32 == low) hi32 = lo32 = 0;
-                }
+                bar = kth_of_threads(sm, best, k, r_th);
+            } else {
                 __syncthreads();
-                if (threadIdx.x < NW * r_th) {
-                    const u64 mine = sm.warp_key[threadIdx.x];
-                    int above = 0;
-#pragma unroll 8
-                    for (int i = 0; i < NW * r_th; ++i) above += sm.warp_key[i] > mine;
-                    if (mine && above == k - 1) sm.bar = mine;
-                }
             }
-            __syncthreads();
-            bar = sm.bar;
             bar_x = bar ? key_value(bar) : -INFINITY;
         }
         if (!(cm < bar_x)) {                                      // (a NaN passes on to the key's comparison)
             uint32_t pass = 0;
 #pragma unroll
-            for (int e = 0; e < C::EPT; ++e) pass |= !(x[e] < bar_x) && (n == C::SIZE || C::column(e) < n) ? 1u << e : 0u;
+            for (int e = 0; e < C::EPT; ++e) pass |= !(x[e] < bar_x) ? 1u << e : 0u;
             for (; pass; pass &= pass - 1) {
                 const int e0 = __ffs(pass) - 1;
+                if (C::column(e0) >= n) break;                    // (columns rise with e: nothing but padding is left)
                 float v = x[0];
 #pragma unroll
                 for (int e = 1; e < C::EPT; ++e) v = e == e0 ? x[e] : v;
@@ -251,14 +293,14 @@ __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int 
         }
     };
     // after a group of chunks: did the list hold, and can the bar be raised?
-    auto look = [&](int g0) {
+    auto look = [&](int g0) __attribute__((always_inline)) {
         const int n = min(GROUP * C::SIZE, hi - g0);
         if (threadIdx.x == 0) sm.count[gi == 2 ? 0 : gi + 1] = 0;
         __syncthreads();
         const int now = count + sm.count[gi];
-        count = now <= LIST ? now : take_largest<T>(sm, row + g0, g0, n, count, k);
+        count = now <= LIST ? now : take_largest<T>(row + g0, g0, n, count, k);
         if (g0 + GROUP * C::SIZE >= hi || count > 2 * k + 16) {
-            count = prune(sm, count, k);
+            count = prune(count, k);
             if (count == k) {
                 bar = sm.list[k - 1];
                 bar_x = key_value(bar);
@@ -282,6 +324,7 @@ __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int 
         look(g0);
     }
     // sums of the threads, in double
+    const float s = s0 + s1;
     float wm = m;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
@@ -303,141 +346,235 @@ __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int 
     return count;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS, 2) beam_kernel(const BeamArgs a) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    Shared &sm = *reinterpret_cast<Shared *>(smem);
-    cg::cluster_group cl = cg::this_cluster();
-    const int rank = cl.block_rank(), n_ranks = cl.num_blocks();
-    const int item = blockIdx.x / n_ranks, beams = a.b.beams, V = a.b.vocab, k = a.b.k, slices = a.slices, n_lists = beams * slices;
-    auto started = cl.barrier_arrive();
-    Shared &first = *cl.map_shared_rank(&sm, 0);
-    // list = beam * slices + slice; with more beams than CTAs (slices = 1) lists rank, rank + n_ranks, ...
-    const int lo = (int)min((int64_t)(rank % slices) * a.slice, (int64_t)V), hi = (int)min((int64_t)lo + a.slice, (int64_t)V);
-    for (int list = rank; list < n_lists; list += n_ranks) {       // (every rank has one)
-        const int row = item * beams + list / slices;
-        float m = -INFINITY;
-        double s = 0.0;
-        int count = 0;
-        if (lo < hi && !(a.b.finished && a.b.finished[row]))
-            count = slice_best<T>(sm, reinterpret_cast<const T *>(a.b.logits) + row * a.b.row_stride, lo, hi, k, a.aligned, m, s);
-        if (list == rank) cl.barrier_wait(std::move(started));    // the first CTA runs: its shared memory may be written
-        for (int i = threadIdx.x; i < k; i += THREADS) first.key[list * k + i] = i < count ? sm.list[i] : 0;
-        if (threadIdx.x == 0) { first.m[list] = m; first.s[list] = s; }
-        __syncthreads();
+// the candidates of an item: k of each of its lists
+struct Cand {
+    u64 *key, *order;                      // order: the scores as numbers in the same order, 0: no candidate
+    double *score, *lse, *cum;             // lse, cum: per beam
+    int32_t *index;                        // of the candidates in the list
+    __device__ Cand(unsigned char *at, int n)
+        : key(reinterpret_cast<u64 *>(at)), order(key + n), score(reinterpret_cast<double *>(order + n)), lse(score + n), cum(lse + MAX_BEAMS),
+          index(reinterpret_cast<int32_t *>(cum + MAX_BEAMS)) {}
+    static constexpr size_t bytes(int n) { return 24 * (size_t)n + 16 * MAX_BEAMS + 4 * LIST; }
+};
+
+// one CTA merges the lists of an item; `wait`: for the kernel that wrote them
+__device__ __forceinline__ void merge(const BeamArgs &a, int item, bool wait) {
+    Shared &sm = shared();
+    const int beams = a.b.beams, V = a.b.vocab, k = a.b.k, slices = a.slices, n_lists = beams * slices, n_cand = n_lists * k;
+    const Cand cd(reinterpret_cast<unsigned char *>(&sm) + (sizeof(Shared) + 15) / 16 * 16, n_cand);
+    double cum = 0.0;
+    bool done = false;
+    if ((int)threadIdx.x < beams) {
+        cum = a.b.scores[item * beams + threadIdx.x];
+        done = a.b.finished && a.b.finished[item * beams + threadIdx.x];
     }
-    if (n_ranks > 1) cl.sync();
-    if (rank != 0) return;
-    // a beam's log-sum-exp; then its lists' scores
-    for (int beam = threadIdx.x; beam < beams; beam += THREADS) {
-        const int row = item * beams + beam;
-        const double cum = a.b.scores[row];
+    if (threadIdx.x == 0) sm.count[0] = 0;
+    if (wait) pdl_wait();
+    const size_t list0 = (size_t)item * n_lists;
+    for (int e = threadIdx.x; e < n_cand; e += THREADS) cd.key[e] = __ldcg(a.key + list0 * k + e);
+    if ((int)threadIdx.x < beams) {
+        // the row's log-sum-exp
         const bool number = cum > -INFINITY && cum < INFINITY;
         double lse = INFINITY;                                    // no candidates but those at -inf; -inf: finished
-        if (a.b.finished && a.b.finished[row]) lse = number ? -INFINITY : INFINITY;
+        if (done) lse = number ? -INFINITY : INFINITY;
         else if (number) {
+            const size_t l0 = list0 + threadIdx.x * slices;
             float M = -INFINITY;
-            for (int r = 0; r < slices; ++r) M = fmaxf(M, sm.m[beam * slices + r]);
+            for (int r = 0; r < slices; ++r) M = fmaxf(M, __ldcg(a.m + l0 + r));
             double S = 0.0;
             for (int r = 0; r < slices; ++r) {
-                const float m = sm.m[beam * slices + r];
-                S += sm.s[beam * slices + r] * (m == -INFINITY ? 1.0 : (double)ex2f((m - M) * LOG2E));
+                const float m = __ldcg(a.m + l0 + r);
+                S += __ldcg(a.s + l0 + r) * (m == -INFINITY ? 1.0 : (double)ex2f((m - M) * LOG2E));
             }
             lse = (double)M + log(S);
             if (!(lse > -INFINITY && lse < INFINITY)) lse = INFINITY;
         }
-        sm.lse[beam] = lse;
+        cd.lse[threadIdx.x] = lse;
+        cd.cum[threadIdx.x] = cum;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < n_lists * k; e += THREADS) {
+    u64 best = 0;
+    for (int e = threadIdx.x; e < n_cand; e += THREADS) {
         const int list = e / k, i = e - list * k, beam = list / slices;
-        const double cum = a.b.scores[item * beams + beam], lse = sm.lse[beam];
-        u64 key = sm.key[e];
+        const double c = cd.cum[beam], lse = cd.lse[beam];
+        u64 key = cd.key[e];
         double score = -INFINITY;
         if (lse == INFINITY || lse == -INFINITY) {
             // one continuation (finished) or none; behind it the lowest tokens at -inf, in the beam's first list
             const int eos = a.b.eos, t = lse == INFINITY ? i : i == 0 ? eos : i - 1 + (i - 1 >= eos);
-            if (lse == -INFINITY && i == 0) score = cum;
-            key = list % slices == 0 && t < V ? make_key(0.f, t) : 0;
+            if (lse == -INFINITY && i == 0) score = c;
+            key = list == beam * slices && t < V ? make_key(0.f, t) : 0;
         } else if (key) {
-            score = cum + ((double)key_value(key) - lse);
+            score = c + ((double)key_value(key) - lse);
         }
-        sm.key[e] = key;
-        sm.score[e] = score;
+        const u64 bits = (u64)__double_as_longlong(score + 0.0), order = key ? (bits >> 63 ? ~bits : bits | (1ull << 63)) : 0;
+        cd.key[e] = key;
+        cd.score[e] = score;
+        cd.order[e] = order;
+        best = max(best, order);
     }
+    // a score that at least k candidates reach, from the threads' best (0, when the threads have fewer than k)
+    const u64 bar = kth_of_threads(sm, best, k, min(32, (k + 3) / 4));
+    for (int e = threadIdx.x; e < n_cand; e += THREADS)
+        if (cd.order[e] && cd.order[e] >= bar) {
+            const int at = atomicAdd(&sm.count[0], 1);
+            if (at < LIST) { sm.list[at] = cd.order[e]; cd.index[at] = e; }
+        }
     __syncthreads();
-    // the lists descend: a candidate's rank is its place plus what the others have before it
-    for (int e = threadIdx.x; e < n_lists * k; e += THREADS) {
-        const u64 key = sm.key[e];
-        if (key == 0) continue;
-        const int list = e / k, beam = list / slices;
-        const double s = sm.score[e];
-        int above = e - list * k;
-        for (int o = 0; o < n_lists && above < k; ++o) {
-            if (o == list) continue;
-            const int ob = o / slices;
-            int n = 0;
-            while (n < k) {
-                const u64 ok = sm.key[o * k + n];
-                const double os = sm.score[o * k + n];
-                if (ok == 0 || !(ob == beam ? ok > key : os > s || (os == s && ob < beam))) break;
-                ++n;
-            }
-            above += n;
+    // those are ranked by counting; where they are too many (equal scores), all are
+    const int n = sm.count[0], total = n <= LIST ? n : n_cand;
+    const u64 *order = n <= LIST ? sm.list : cd.order;
+    for (int c = threadIdx.x; c < total; c += THREADS) {
+        const u64 mine = order[c];
+        if (!mine) continue;
+        int above = 0, equal = 0;
+#pragma unroll 8
+        for (int o = 0; o < total; ++o) {
+            above += order[o] > mine;
+            equal += order[o] == mine;
+        }
+        if (above >= k) continue;
+        const int e = n <= LIST ? cd.index[c] : c, beam = e / k / slices;
+        const u64 key = cd.key[e];
+        for (int o = 0; equal > 1 && o < total; ++o) {
+            if (order[o] != mine || o == c) continue;
+            const int e2 = n <= LIST ? cd.index[o] : o, b2 = e2 / k / slices;
+            above += b2 < beam || (b2 == beam && cd.key[e2] > key);
         }
         if (above < k) {
             const size_t at = (size_t)item * k + above;
-            a.b.out_scores[at] = (float)s;
+            a.b.out_scores[at] = (float)cd.score[e];
             a.b.out_tokens[at] = key_token(key);
             a.b.out_rows[at] = item * beams + beam;
         }
     }
 }
 
-template <typename T>
-cudaError_t launch(const BeamArgs &a, int ranks, cudaStream_t st) {
-    auto kern = beam_kernel<T>;
-    static SmemAttrOnce attr;
-    static bool big[DEL_MAX_DEVICES] = {};
-    cudaError_t e = attr.set(kern, (int)sizeof(Shared));
-    int dev = 0;
-    if (e == cudaSuccess) e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (!(dev < DEL_MAX_DEVICES && big[dev])) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        if (dev < DEL_MAX_DEVICES) big[dev] = true;
+template <typename T, bool FUSED>
+__global__ void __launch_bounds__(THREADS, 1) beam_slice_kernel(const BeamArgs a) {
+    Shared &sm = shared();
+    const int row = blockIdx.y, k = a.b.k, list = row * a.slices + blockIdx.x;
+    const int lo = (int)min((int64_t)blockIdx.x * a.slice, (int64_t)a.b.vocab), hi = (int)min((int64_t)lo + a.slice, (int64_t)a.b.vocab);
+    if (!FUSED) pdl_launch();
+    float m = -INFINITY;
+    double s = 0.0;
+    int count = 0;
+    if (lo < hi && !(a.b.finished && a.b.finished[row]))
+        count = slice_best<T>(sm, reinterpret_cast<const T *>(a.b.logits) + row * a.b.row_stride, lo, hi, k, a.aligned, m, s);
+    for (int i = threadIdx.x; i < k; i += THREADS) a.key[(size_t)list * k + i] = i < count ? sm.list[i] : 0;
+    if (threadIdx.x == 0) { a.m[list] = m; a.s[list] = s; }
+    if (FUSED) {
+        cooperative_groups::this_cluster().sync();                // the item's lists are written
+        if (blockIdx.x == 0 && row % a.b.beams == 0) merge(a, row / a.b.beams, false);
     }
-    return launch_cluster(kern, dim3(a.b.batch * ranks), THREADS, sizeof(Shared), ranks, st, a);
+}
+
+__global__ void __launch_bounds__(THREADS) beam_merge_kernel(const BeamArgs a) { merge(a, blockIdx.x, true); }
+
+template <typename T>
+cudaError_t launch(const BeamArgs &a, cudaStream_t st) {
+    constexpr size_t fixed = (sizeof(Shared) + 15) / 16 * 16;
+    const size_t merge_bytes = fixed + Cand::bytes(a.b.beams * a.slices * a.b.k);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.gridDim = dim3(a.slices, a.b.batch * a.b.beams);
+    if (a.fused) {
+        static SmemAttrOnce attr;
+        static bool big[DEL_MAX_DEVICES] = {};
+        auto kern = beam_slice_kernel<T, true>;
+        cudaError_t e = attr.set(kern, (int)(fixed + Cand::bytes(MAX_CLUSTER * MAX_K)));
+        int dev = 0;
+        if (e == cudaSuccess) e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (a.slices * a.b.beams > 8 && !(dev < DEL_MAX_DEVICES && big[dev])) {
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (e != cudaSuccess) return e;
+            if (dev < DEL_MAX_DEVICES) big[dev] = true;
+        }
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = a.slices;
+        at[0].val.clusterDim.y = a.b.beams;
+        at[0].val.clusterDim.z = 1;
+        cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = merge_bytes;
+        return cudaLaunchKernelEx(&cfg, kern, a);
+    }
+    cfg.dynamicSmemBytes = sizeof(Shared);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, beam_slice_kernel<T, false>, a);
+    if (e != cudaSuccess) return e;
+    static SmemAttrOnce attr;
+    e = attr.set(beam_merge_kernel, (int)(fixed + Cand::bytes(MAX_CAND)));
+    if (e != cudaSuccess) return e;
+    // (the second kernel's CTAs are few and short: they start while the first drains, and wait for its end before they read)
+    cfg.gridDim = dim3(a.b.batch);
+    cfg.dynamicSmemBytes = merge_bytes;
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, beam_merge_kernel, a);
+}
+
+// CTAs per row: as many over all rows as the device has SMs, none with less than 2048 columns (a smaller slice is all latency),
+// and no more candidates of an item than the merge holds
+int slices_of(const del_beam &x, int n_sms) {
+    int64_t n = n_sms / ((int64_t)x.batch * x.beams);
+    const int64_t most = (x.vocab + 2047) / 2048, held = MAX_CAND / ((int64_t)x.beams * x.k);
+    n = n < most ? n : most;
+    n = n < held ? n : held;
+    return n < 1 ? 1 : (int)n;
+}
+
+// The one-launch form: slices per row such that an item is a cluster, all of which are resident, and no slice is longer than what
+// a second launch costs (about 32768 columns, 6 us); 0: two launches
+int fused_slices(const del_beam &x) {
+    if (x.beams > MAX_CLUSTER) return 0;
+    const int most = (x.vocab + 2047) / 2048, n = MAX_CLUSTER / x.beams < most ? MAX_CLUSTER / x.beams : most;
+    return x.batch <= (n * x.beams <= 8 ? 15 : 7) && x.vocab / n <= 32768 ? n : 0;
+}
+
+bool valid(const del_beam *x) {
+    if (!x || (x->dtype != DEL_F32 && x->dtype != DEL_BF16 && x->dtype != DEL_F16)) return false;
+    if (x->batch < 1 || x->batch > 65535 || x->beams < 1 || x->beams > MAX_BEAMS || x->vocab < 1 || x->vocab > (1 << 30)) return false;
+    return x->k >= 1 && x->k <= MAX_K && (int64_t)x->beams * x->vocab >= x->k && (int64_t)x->batch * x->beams <= 65535;
+}
+
+// slices_of gives at most n_sms lists, or one per row, fused_slices at most 120: enough for any device of up to 1024 SMs
+size_t workspace_bytes(const del_beam &x) {
+    const size_t rows = (size_t)x.batch * x.beams, lists = rows > 1024 ? rows : 1024;
+    return lists * (8 * (size_t)x.k + 16);
 }
 
 }  // namespace
 
+extern "C" size_t del_beam_workspace_bytes(const del_beam *x) {
+    return valid(x) ? workspace_bytes(*x) : 0;
+}
+
 extern "C" int del_beam_select(const del_beam *x, void *cuda_stream) {
-    if (!x || !x->logits || !x->scores || !x->out_scores || !x->out_tokens || !x->out_rows) return DEL_EINVAL;
-    if (x->dtype != DEL_F32 && x->dtype != DEL_BF16 && x->dtype != DEL_F16) return DEL_EINVAL;
+    if (!valid(x) || !x->logits || !x->scores || !x->out_scores || !x->out_tokens || !x->out_rows || !x->workspace) return DEL_EINVAL;
     const int size = x->dtype == DEL_F32 ? 4 : 2;
     if (((uintptr_t)x->scores | (uintptr_t)x->out_scores | (uintptr_t)x->out_tokens | (uintptr_t)x->out_rows) & 3 || (uintptr_t)x->logits % size) return DEL_EINVAL;
-    if (x->batch < 1 || x->batch > (1 << 20) || x->beams < 1 || x->beams > MAX_BEAMS || x->vocab < 1 || x->vocab > (1 << 30)) return DEL_EINVAL;
-    if (x->k < 1 || x->k > MAX_K || (int64_t)x->beams * x->vocab < x->k || x->row_stride < x->vocab) return DEL_EINVAL;
-    if ((int64_t)x->batch * x->beams > INT32_MAX) return DEL_EINVAL;
+    if ((uintptr_t)x->workspace & 15 || x->row_stride < x->vocab) return DEL_EINVAL;
     if (x->finished && (x->eos < 0 || x->eos >= x->vocab)) return DEL_EINVAL;
     const int n_sms = current_sms();
-    if (!n_sms) return DEL_ECUDA;
+    if (!n_sms || n_sms > 1024) return DEL_ECUDA;
     BeamArgs a;
     memset(&a, 0, sizeof(a));
     a.b = *x;
     a.aligned = ((uintptr_t)x->logits & 15) == 0 && (x->row_stride * size) % 16 == 0;
-    // CTAs per item: two per SM over all items, at most 16 (a cluster), none with less than 2048 columns (a smaller slice is all
-    // latency); whole rows per CTA where there are more beams than CTAs
-    int64_t ranks = 2 * (int64_t)n_sms / x->batch, most = (int64_t)x->beams * ((x->vocab + 2047) / 2048);
-    if (ranks > (x->batch <= 6 ? MAX_CLUSTER : 8)) ranks = x->batch <= 6 ? MAX_CLUSTER : 8;
-    if (ranks > most) ranks = most;
-    if (ranks < 1) ranks = 1;
-    a.slices = ranks >= x->beams ? (int)(ranks / x->beams) : 1;
-    if (ranks >= x->beams) ranks = (int64_t)a.slices * x->beams;
+    a.slices = fused_slices(*x);
+    a.fused = a.slices > 0;
+    if (!a.fused) a.slices = slices_of(*x, n_sms);
     a.slice = ((x->vocab + a.slices - 1) / a.slices + 7) / 8 * 8;
+    if (x->workspace_bytes < workspace_bytes(*x)) return DEL_ENOSPC;
+    const size_t lists = (size_t)x->batch * x->beams * a.slices;
+    a.key = (u64 *)x->workspace;
+    a.s = (double *)(a.key + lists * x->k);
+    a.m = (float *)(a.s + lists);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const cudaError_t e = x->dtype == DEL_F32 ? launch<float>(a, (int)ranks, st) : x->dtype == DEL_BF16 ? launch<bf16>(a, (int)ranks, st) : launch<__half>(a, (int)ranks, st);
+    const cudaError_t e = x->dtype == DEL_F32 ? launch<float>(a, st) : x->dtype == DEL_BF16 ? launch<bf16>(a, st) : launch<__half>(a, st);
     return e == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }

@@ -31,7 +31,7 @@ COMPACT = dict(src_table=P, dst_table=P, src_pos=P, counts=P, dst_start=P, batch
                dst_stride=4, pos_stride=4)
 FORK = dict(table=P, lens=P, parents=P, spare=P, n_spare=P, new_table=2 * P, new_lens=2 * P, free_pages=None, counts=3 * P, n_old=2, n_new=2,
             old_cols=4, old_stride=4, new_cols=4, new_stride=4, spare_cap=4, room=1)
-BEAM = dict(logits=P, scores=P, finished=None, out_scores=P, out_tokens=P, out_rows=P, row_stride=100, batch=2, beams=3, vocab=100, k=4, eos=0, dtype=0)
+BEAM = dict(logits=P, scores=P, finished=None, out_scores=P, out_tokens=P, out_rows=P, workspace=P, workspace_bytes=1 << 20, row_stride=100, batch=2, beams=3, vocab=100, k=4, eos=0, dtype=0)
 
 BAD_PAGES = [dict(k_pages=None), dict(v_pages=P + 8), dict(n_pages=0), dict(n_layers=0), dict(n_kv_heads=0), dict(head_dim=96)]
 
@@ -65,7 +65,8 @@ def test_fork_refuses_to_list_more_pages_than_it_can_mark():
     assert call("del_kv_fork", dl.ForkC, FORK, dict(free_pages=64 * P), dict(n_pages=(1 << 20) + 1)) == dl.EINVAL
 
 
-@pytest.mark.parametrize("over", [dict(logits=None), dict(scores=None), dict(out_scores=None), dict(out_tokens=None), dict(out_rows=None), dict(logits=P + 2),
+@pytest.mark.parametrize("over", [dict(logits=None), dict(scores=None), dict(out_scores=None), dict(out_tokens=None), dict(out_rows=None), dict(logits=P + 2), dict(workspace=None), dict(workspace=P + 8),
+                                  dict(batch=65536), dict(batch=2000, beams=64),
                                   dict(dtype=3), dict(dtype=-1), dict(batch=0), dict(beams=0), dict(beams=65), dict(vocab=0), dict(k=0), dict(k=65),
                                   dict(vocab=1, row_stride=1), dict(row_stride=99), dict(finished=P, eos=100), dict(finished=P, eos=-1)])
 def test_beam_select_refuses(over):
