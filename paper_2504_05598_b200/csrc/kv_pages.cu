@@ -8,64 +8,159 @@ namespace {
 
 // ---------------------------------------------------------------- compaction
 //
-// One CTA moves all positions of one (row, layer, kv head), CHUNK of them at a time in ascending order: sources into shared
-// memory, barrier, then out.  A chunk's sources are read before anything of it is written, and with src_pos ascending and never
-// behind its destination, no earlier chunk has written what a later one reads: in-place moves need no second buffer.
-constexpr int CP_THREADS = 256, CHUNK = 32;
+// One CTA moves all positions of one (row, layer, kv head), a warp a destination page at a time, in rounds: every warp reads what its
+// page gets into registers, barrier, then out.  With src_pos ascending and never behind its destination, a page written in this round
+// holds no source of a later page, and the sources that earlier pages had in it have been read: in-place moves need no second buffer.
+// (Pages are therefore not spread over CTAs; layers x kv heads x rows are enough of them.)
+//
+// A key is a row of hd values: 16-byte copies.  Values lie transposed, 16 tokens in 32 bytes: the source pages' blocks are copied whole
+// into shared memory, a lane picks the tokens of its dimensions in the order of their destinations and writes 32-byte rows (two bytes at a
+// time where a destination page is only partly written).  So values are read by whole source pages: of contexts kept by halves, 5
+// bytes move where 4 would do.  The copies are asynchronous and one round ahead, page ids two rounds, positions three: a round would
+// otherwise wait for three to five round trips to memory in turn (2 x 4 003 of 8 001 positions, 1B shape: 165 us that way).
+constexpr int CP_WARPS = 4, CP_RUNS = 6;       // source pages of a destination page that are staged; what comes from further ones is loaded directly
 
 struct CompactArgs {
     PageView kv;
     del_compact c;
 };
 
+// 16-bit element `slot` of a 32-byte row
+__device__ __forceinline__ uint32_t pick(const uint4 (&r)[2], int slot) {
+    const bool h = slot & 8, w2 = slot & 4, w1 = slot & 2;
+    const uint32_t a = h ? r[1].x : r[0].x, b = h ? r[1].y : r[0].y, c = h ? r[1].z : r[0].z, d = h ? r[1].w : r[0].w;
+    const uint32_t e = w2 ? c : a, f = w2 ? d : b, g = w1 ? f : e;
+    return slot & 1 ? g >> 16 : g & 0xffffu;
+}
+
+template <int HD> struct Compact {
+    static constexpr int K_BYTES = 16 * HD * 2, V_BYTES = HD * 32, WARP = 2 * (K_BYTES + CP_RUNS * V_BYTES);      // two rounds per warp
+};
+
 template <int HD>
-__global__ void __launch_bounds__(CP_THREADS) compact_kernel(const CompactArgs a) {
-    __shared__ __align__(16) bf16 sk[CHUNK][HD];
-    __shared__ bf16 sv[HD][CHUNK + 2];
-    __shared__ int64_t src_page[CHUNK], dst_page[CHUNK];      // element offset of the (page, layer, head) block, -1: not moved
-    __shared__ int src_slot[CHUNK], dst_slot[CHUNK];
-    const int b = blockIdx.y;
+__global__ void __launch_bounds__(CP_WARPS * 32) compact_kernel(const CompactArgs a) {
+    using C = Compact<HD>;
+    extern __shared__ __align__(16) unsigned char smem[];
+    constexpr int DPL = HD / 32;                                // dimensions per lane
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5, b = blockIdx.y;
     const int n = min(max(a.c.counts[b], 0), a.c.max_count);
-    const int start = a.c.dst_start[b];
+    const int64_t start = a.c.dst_start[b], first_page = start >= 0 ? start >> 4 : -((-start + 15) >> 4);
+    const int64_t n_pages = n > 0 ? ((start + n - 1) >> 4) - first_page + 1 : 0;
     const size_t head = (size_t)blockIdx.x * a.kv.head_elems(), page_elems = a.kv.page_elems();
-    for (int i0 = 0; i0 < n; i0 += CHUNK) {
-        if (threadIdx.x < CHUNK) {
-            const int i = i0 + threadIdx.x;
-            int64_t s = -1, d = -1;
-            if (i < n) {
-                const int64_t sp = a.c.src_pos[(size_t)b * a.c.pos_stride + i], dp = (int64_t)start + i;
-                if (sp >= 0 && sp < (int64_t)a.c.src_cols * 16 && dp >= 0 && dp < (int64_t)a.c.dst_cols * 16) {
-                    const int spg = a.c.src_table[(size_t)b * a.c.src_stride + (sp >> 4)], dpg = a.c.dst_table[(size_t)b * a.c.dst_stride + (dp >> 4)];
-                    if (a.kv.holds(spg) && a.kv.holds(dpg)) {
-                        s = (int64_t)((size_t)spg * page_elems + head);
-                        d = (int64_t)((size_t)dpg * page_elems + head);
-                        src_slot[threadIdx.x] = (int)(sp & 15);
-                        dst_slot[threadIdx.x] = (int)(dp & 15);
+    // lane j < 16 looks after slot j of the warp's destination page
+    auto position = [&](int64_t p0) -> int {                     // source position of the lane's slot, -1: none
+        const int64_t dp = first_page + p0 + warp, i = dp * 16 + lane - start;
+        return p0 + warp < n_pages && dp >= 0 && dp < a.c.dst_cols && lane < 16 && i >= 0 && i < n ? a.c.src_pos[(size_t)b * a.c.pos_stride + i] : -1;
+    };
+    struct From { int src, dst, slot; uint32_t moved, runs; };   // source page of the lane's slot, destination page; slots that are written, that begin a source page
+    auto ids = [&](int64_t p0, int sp, From &f) {
+        const int64_t dp = first_page + p0 + warp;
+        f.dst = p0 + warp < n_pages && dp >= 0 && dp < a.c.dst_cols ? a.c.dst_table[(size_t)b * a.c.dst_stride + dp] : -1;
+        f.src = sp >= 0 && sp < (int64_t)a.c.src_cols * 16 ? a.c.src_table[(size_t)b * a.c.src_stride + (sp >> 4)] : -1;
+        f.slot = sp & 15;
+    };
+    unsigned char *mine = smem + warp * C::WARP;
+    auto fetch = [&](From &f, int stage) {                       // requests the round's keys and values
+        if (!a.kv.holds(f.dst)) f.dst = -1;
+        if (f.dst < 0 || !a.kv.holds(f.src)) f.src = -1;
+        f.moved = __ballot_sync(0xffffffffu, f.src >= 0);
+        const int before = __shfl_up_sync(0xffffffffu, f.src, 1);
+        f.runs = __ballot_sync(0xffffffffu, lane < 16 && f.src >= 0 && (lane == 0 || f.src != before));
+        unsigned char *ks = mine + stage * (C::WARP / 2), *vs = ks + C::K_BYTES;
+        if (f.moved) {
+#pragma unroll
+            for (int v = 0; v < C::K_BYTES / 512; ++v) {
+                const int piece = v * 32 + lane, j = piece / (HD / 8), c = piece % (HD / 8) * 8;
+                const int pg = __shfl_sync(0xffffffffu, f.src, j), sl = __shfl_sync(0xffffffffu, f.slot, j);
+                if (pg >= 0) cp_async16(ks + piece * 16, a.kv.k + (size_t)pg * page_elems + head + sl * HD + c, true);
+            }
+            uint32_t left = f.runs;
+            for (int r = 0; r < CP_RUNS && left; ++r, left &= left - 1) {
+                const int pg = __shfl_sync(0xffffffffu, f.src, __ffs(left) - 1);
+                const bf16 *v = a.kv.v + (size_t)pg * page_elems + head;
+#pragma unroll
+                for (int i = 0; i < C::V_BYTES / 512; ++i) cp_async16(vs + r * C::V_BYTES + (i * 32 + lane) * 16, v + (i * 32 + lane) * 8, true);
+            }
+        }
+        cp_async_commit();
+    };
+    From cur, nxt;
+    int pos1 = position(0), pos2 = position(n_warps);
+    ids(0, pos1, nxt);
+    pos1 = pos2;
+    pos2 = position(2 * n_warps);
+    fetch(nxt, 0);
+    cur = nxt;
+    ids(n_warps, pos1, nxt);
+    int stage = 0;
+    for (int64_t p0 = 0; p0 < n_pages; p0 += n_warps, stage ^= 1) {
+        fetch(nxt, stage ^ 1);                                    // (behind the last round: nothing)
+        From later;
+        ids(p0 + 2 * n_warps, pos2, later);
+        pos2 = position(p0 + 3 * n_warps);
+        cp_async_wait<1>();
+        __syncwarp();
+        const unsigned char *ks = mine + stage * (C::WARP / 2), *vs = ks + C::K_BYTES;
+        uint32_t vals[DPL][8];
+        if (cur.moved) {
+            uint4 rows[DPL][2];
+            int run = -1;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if ((cur.runs >> j) & 1) {
+                    ++run;
+                    if (run < CP_RUNS) {
+#pragma unroll
+                        for (int d = 0; d < DPL; ++d) {
+                            const uint4 *r = reinterpret_cast<const uint4 *>(vs + run * C::V_BYTES + (lane + d * 32) * 32);
+                            rows[d][0] = r[0];
+                            rows[d][1] = r[1];
+                        }
+                    } else {
+                        const bf16 *v = a.kv.v + (size_t)__shfl_sync(0xffffffffu, cur.src, j) * page_elems + head + (size_t)lane * 16;
+#pragma unroll
+                        for (int d = 0; d < DPL; ++d) {
+                            rows[d][0] = *reinterpret_cast<const uint4 *>(v + d * 512);
+                            rows[d][1] = *reinterpret_cast<const uint4 *>(v + d * 512 + 8);
+                        }
                     }
                 }
+                const int sl = __shfl_sync(0xffffffffu, cur.slot, j);
+#pragma unroll
+                for (int d = 0; d < DPL; ++d) {
+                    const uint32_t x = pick(rows[d], sl);         // (of a slot that stays: never written)
+                    vals[d][j >> 1] = j & 1 ? vals[d][j >> 1] | (x << 16) : x;
+                }
             }
-            src_page[threadIdx.x] = s;
-            dst_page[threadIdx.x] = d;
         }
-        __syncthreads();
-        for (int e = threadIdx.x; e < CHUNK * (HD / 8); e += CP_THREADS) {
-            const int i = e / (HD / 8), c = e % (HD / 8) * 8;
-            if (src_page[i] >= 0) *reinterpret_cast<uint4 *>(&sk[i][c]) = *reinterpret_cast<const uint4 *>(a.kv.k + src_page[i] + src_slot[i] * HD + c);
+        __syncthreads();                                          // every page of the round has been read
+        if (cur.moved) {
+            bf16 *kd = a.kv.k + (size_t)cur.dst * page_elems + head, *vd = a.kv.v + (size_t)cur.dst * page_elems + head + (size_t)lane * 16;
+#pragma unroll
+            for (int v = 0; v < C::K_BYTES / 512; ++v) {
+                const int piece = v * 32 + lane;
+                if ((cur.moved >> (piece / (HD / 8))) & 1) *reinterpret_cast<uint4 *>(kd + piece * 8) = *reinterpret_cast<const uint4 *>(ks + piece * 16);
+            }
+            if (cur.moved == 0xffffu) {
+#pragma unroll
+                for (int d = 0; d < DPL; ++d) {
+                    *reinterpret_cast<uint4 *>(vd + d * 512) = make_uint4(vals[d][0], vals[d][1], vals[d][2], vals[d][3]);
+                    *reinterpret_cast<uint4 *>(vd + d * 512 + 8) = make_uint4(vals[d][4], vals[d][5], vals[d][6], vals[d][7]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if ((cur.moved >> j) & 1)
+#pragma unroll
+                        for (int d = 0; d < DPL; ++d)
+                            reinterpret_cast<uint16_t *>(vd + d * 512)[j] = (uint16_t)(j & 1 ? vals[d][j >> 1] >> 16 : vals[d][j >> 1]);
+            }
         }
-        for (int e = threadIdx.x; e < CHUNK * HD; e += CP_THREADS) {
-            const int i = e % CHUNK, c = e / CHUNK;
-            if (src_page[i] >= 0) sv[c][i] = a.kv.v[src_page[i] + c * 16 + src_slot[i]];
-        }
-        __syncthreads();
-        for (int e = threadIdx.x; e < CHUNK * (HD / 8); e += CP_THREADS) {
-            const int i = e / (HD / 8), c = e % (HD / 8) * 8;
-            if (dst_page[i] >= 0) *reinterpret_cast<uint4 *>(a.kv.k + dst_page[i] + dst_slot[i] * HD + c) = *reinterpret_cast<const uint4 *>(&sk[i][c]);
-        }
-        for (int e = threadIdx.x; e < CHUNK * HD; e += CP_THREADS) {
-            const int i = e % CHUNK, c = e / CHUNK;
-            if (dst_page[i] >= 0) a.kv.v[dst_page[i] + c * 16 + dst_slot[i]] = sv[c][i];
-        }
-        __syncthreads();
+        // (The next rounds' sources, some of them read already, lie behind this round's destinations, or in pages that are not
+        // written: no second barrier.)
+        __syncwarp();                                             // the stage may be filled again
+        cur = nxt;
+        nxt = later;
     }
 }
 
@@ -170,8 +265,8 @@ __global__ void __launch_bounds__(FK_THREADS) fork_kernel(const ForkArgs a) {
             const int words = (a.kv.n_pages + 31) >> 5;
             for (int w = threadIdx.x; w < words; w += FK_THREADS) used_bits[w] = 0;
             __syncthreads();
-            for (int b = 0; b < f.n_new; ++b)
-                for (int p = threadIdx.x; p < row_wanted[b]; p += FK_THREADS) {
+            for (int b = threadIdx.x >> 5; b < f.n_new; b += FK_THREADS / 32)       // a row per warp
+                for (int p = threadIdx.x & 31; p < row_wanted[b]; p += 32) {
                     const int pg = entry(b, p);
                     if (a.kv.holds(pg)) atomicOr(&used_bits[pg >> 5], 1u << (pg & 31));
                 }
@@ -191,18 +286,28 @@ __global__ void __launch_bounds__(FK_THREADS) fork_kernel(const ForkArgs a) {
         }
         if (threadIdx.x == 0) { f.counts[0] = before; f.counts[1] = n_missing; }
     }
-    // pieces of the pages to copy, keys and values
+    // pieces of the pages to copy, keys and values: large ones, four loads of a thread in flight, where there are enough of them
     const size_t page_bytes = a.kv.page_elems() * sizeof(bf16);
-    const int per_page = (int)((page_bytes + PIECE - 1) / PIECE);
+    const bool large = (int64_t)n_copies * 2 * (int64_t)(page_bytes / (4 * PIECE)) >= n_cta;
+    const size_t piece = large ? 4 * PIECE : PIECE;
+    const int per_page = (int)((page_bytes + piece - 1) / piece);
     const int64_t items = (int64_t)n_copies * per_page * 2;
     for (int64_t it = blockIdx.x; it < items; it += n_cta) {
         const int c = (int)(it / (per_page * 2)), q = (int)(it % (per_page * 2));
         char *pool = reinterpret_cast<char *>(q < per_page ? a.kv.k : a.kv.v);
-        const size_t off = (size_t)(q < per_page ? q : q - per_page) * PIECE;
+        const size_t off = (size_t)(q < per_page ? q : q - per_page) * piece;
         const uint4 *s = reinterpret_cast<const uint4 *>(pool + copy_src[c] * page_bytes + off);
         uint4 *d = reinterpret_cast<uint4 *>(pool + copy_dst[c] * page_bytes + off);
-        const int n = (int)(min((size_t)PIECE, page_bytes - off) / 16);
-        for (int e = threadIdx.x; e < n; e += FK_THREADS) d[e] = s[e];
+        const int n = (int)(min(piece, page_bytes - off) / 16);
+        if (n == 4 * FK_THREADS) {
+            uint4 v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __ldcs(s + e * FK_THREADS + threadIdx.x);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) __stcs(d + e * FK_THREADS + threadIdx.x, v[e]);
+        } else {
+            for (int e = threadIdx.x; e < n; e += FK_THREADS) d[e] = s[e];
+        }
     }
 }
 
@@ -221,10 +326,15 @@ extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *c
     if (x->batch < 1 || x->batch > 65535 || x->max_count < 1 || x->src_cols < 1 || x->dst_cols < 1) return DEL_EINVAL;
     if (x->src_stride < 0 || x->dst_stride < 0 || x->pos_stride < 0) return DEL_EINVAL;
     a.c = *x;
-    const dim3 grid(a.kv.L * a.kv.nkv, x->batch);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (a.kv.hd == 128) compact_kernel<128><<<grid, CP_THREADS, 0, st>>>(a);
-    else compact_kernel<64><<<grid, CP_THREADS, 0, st>>>(a);
+    // a warp for each destination page of a round: positions of up to max_count / 16 + 1 pages
+    const dim3 grid(a.kv.L * a.kv.nkv, x->batch);
+    const int warps = (x->max_count + 14) / 16 + 1 < CP_WARPS ? (x->max_count + 14) / 16 + 1 : CP_WARPS;
+    static SmemAttrOnce attr128, attr64;
+    if ((a.kv.hd == 128 ? attr128.set(compact_kernel<128>, CP_WARPS * Compact<128>::WARP) : attr64.set(compact_kernel<64>, CP_WARPS * Compact<64>::WARP)) != cudaSuccess)
+        return DEL_ECUDA;
+    if (a.kv.hd == 128) compact_kernel<128><<<grid, warps * 32, warps * Compact<128>::WARP, st>>>(a);
+    else compact_kernel<64><<<grid, warps * 32, warps * Compact<64>::WARP, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }
 
