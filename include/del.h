@@ -362,9 +362,10 @@ int del_tree_attention(const del_pages *kv, const del_tree_attn *args, void *cud
 
 /* Moves cached positions of all layers and heads: position dst_start[b] + i of dst_table's row b becomes position src_pos[b][i] of
  * src_table's row b, for i < counts[b] (at most max_count).  Commits the accepted path of a draft tree (src_table = dst_table,
- * src_pos = lens + path, dst_start = lens), or compacts the kept positions of a context into other pages.  A row's sources and
- * destinations may overlap if src_pos[b] ascends strictly and src_pos[b][i] >= dst_start[b] + i; otherwise no position written may be
- * one that is read, nor may two rows write the same one.  A position outside its table (src_cols * 16, dst_cols * 16) or on a
+ * src_pos = lens + path, dst_start = lens), or compacts the kept positions of a context into other pages.  In place (src_table and
+ * dst_table the same pointer) a row's sources and destinations may overlap if src_pos[b] ascends strictly and src_pos[b][i] >=
+ * dst_start[b] + i; otherwise no position written may be one that is read.  No position may be written twice.  A position outside its table
+ * (src_cols * 16, dst_cols * 16) or on a
  * page id outside [0, n_pages) is not moved. */
 typedef struct {
     const int32_t *src_table, *dst_table;    /* [batch] rows of src_cols / dst_cols entries, src_stride / dst_stride apart */

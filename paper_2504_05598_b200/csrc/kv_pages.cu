@@ -11,18 +11,20 @@ namespace {
 // One CTA moves all positions of one (row, layer, kv head), a warp a destination page at a time, in rounds: every warp reads what its
 // page gets into registers, barrier, then out.  With src_pos ascending and never behind its destination, a page written in this round
 // holds no source of a later page, and the sources that earlier pages had in it have been read: in-place moves need no second buffer.
-// (Pages are therefore not spread over CTAs; layers x kv heads x rows are enough of them.)
+// Moves between two tables have no order: there a row's pages are spread over further CTAs (about six per SM, which evens out what
+// two or three large ones per SM leave idle, and fills the GPU at all where layers x kv heads x rows are few).
 //
 // A key is a row of hd values: 16-byte copies.  Values lie transposed, 16 tokens in 32 bytes: the source pages' blocks are copied whole
 // into shared memory, a lane picks the tokens of its dimensions in the order of their destinations and writes 32-byte rows (two bytes at a
 // time where a destination page is only partly written).  So values are read by whole source pages: of contexts kept by halves, 5
 // bytes move where 4 would do.  The copies are asynchronous and one round ahead, page ids two rounds, positions three: a round would
 // otherwise wait for three to five round trips to memory in turn (2 x 4 003 of 8 001 positions, 1B shape: 165 us that way).
-constexpr int CP_WARPS = 4, CP_RUNS = 6;       // source pages of a destination page that are staged; what comes from further ones is loaded directly
+constexpr int CP_WARPS = 4, CP_RUNS = 2;       // source pages of a destination page that are staged; what comes from further ones is loaded directly
 
 struct CompactArgs {
     PageView kv;
     del_compact c;
+    int32_t stages;            // 2; 1 where every part is a single round
 };
 
 // 16-bit element `slot` of a 32-byte row
@@ -34,18 +36,19 @@ __device__ __forceinline__ uint32_t pick(const uint4 (&r)[2], int slot) {
 }
 
 template <int HD> struct Compact {
-    static constexpr int K_BYTES = 16 * HD * 2, V_BYTES = HD * 32, WARP = 2 * (K_BYTES + CP_RUNS * V_BYTES);      // two rounds per warp
+    static constexpr int K_BYTES = 16 * HD * 2, V_BYTES = HD * 32, STAGE = K_BYTES + CP_RUNS * V_BYTES;      // a warp's page of a round
 };
 
 template <int HD>
-__global__ void __launch_bounds__(CP_WARPS * 32) compact_kernel(const CompactArgs a) {
+__global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const CompactArgs a) {
     using C = Compact<HD>;
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr int DPL = HD / 32;                                // dimensions per lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5, b = blockIdx.y;
     const int n = min(max(a.c.counts[b], 0), a.c.max_count);
     const int64_t start = a.c.dst_start[b], first_page = start >= 0 ? start >> 4 : -((-start + 15) >> 4);
-    const int64_t n_pages = n > 0 ? ((start + n - 1) >> 4) - first_page + 1 : 0;
+    const int64_t all_pages = n > 0 ? ((start + n - 1) >> 4) - first_page + 1 : 0;
+    const int64_t per_part = (all_pages + gridDim.z - 1) / gridDim.z, p_first = per_part * blockIdx.z, n_pages = min(all_pages, p_first + per_part);
     const size_t head = (size_t)blockIdx.x * a.kv.head_elems(), page_elems = a.kv.page_elems();
     // lane j < 16 looks after slot j of the warp's destination page
     auto position = [&](int64_t p0) -> int {                     // source position of the lane's slot, -1: none
@@ -59,14 +62,14 @@ __global__ void __launch_bounds__(CP_WARPS * 32) compact_kernel(const CompactArg
         f.src = sp >= 0 && sp < (int64_t)a.c.src_cols * 16 ? a.c.src_table[(size_t)b * a.c.src_stride + (sp >> 4)] : -1;
         f.slot = sp & 15;
     };
-    unsigned char *mine = smem + warp * C::WARP;
+    unsigned char *mine = smem + warp * a.stages * C::STAGE;
     auto fetch = [&](From &f, int stage) {                       // requests the round's keys and values
         if (!a.kv.holds(f.dst)) f.dst = -1;
         if (f.dst < 0 || !a.kv.holds(f.src)) f.src = -1;
         f.moved = __ballot_sync(0xffffffffu, f.src >= 0);
         const int before = __shfl_up_sync(0xffffffffu, f.src, 1);
         f.runs = __ballot_sync(0xffffffffu, lane < 16 && f.src >= 0 && (lane == 0 || f.src != before));
-        unsigned char *ks = mine + stage * (C::WARP / 2), *vs = ks + C::K_BYTES;
+        unsigned char *ks = mine + stage * C::STAGE, *vs = ks + C::K_BYTES;
         if (f.moved) {
 #pragma unroll
             for (int v = 0; v < C::K_BYTES / 512; ++v) {
@@ -85,22 +88,22 @@ __global__ void __launch_bounds__(CP_WARPS * 32) compact_kernel(const CompactArg
         cp_async_commit();
     };
     From cur, nxt;
-    int pos1 = position(0), pos2 = position(n_warps);
-    ids(0, pos1, nxt);
+    int pos1 = position(p_first), pos2 = position(p_first + n_warps);
+    ids(p_first, pos1, nxt);
     pos1 = pos2;
-    pos2 = position(2 * n_warps);
+    pos2 = position(p_first + 2 * n_warps);
     fetch(nxt, 0);
     cur = nxt;
-    ids(n_warps, pos1, nxt);
+    ids(p_first + n_warps, pos1, nxt);
     int stage = 0;
-    for (int64_t p0 = 0; p0 < n_pages; p0 += n_warps, stage ^= 1) {
+    for (int64_t p0 = p_first; p0 < n_pages; p0 += n_warps, stage ^= 1) {
         fetch(nxt, stage ^ 1);                                    // (behind the last round: nothing)
         From later;
         ids(p0 + 2 * n_warps, pos2, later);
         pos2 = position(p0 + 3 * n_warps);
         cp_async_wait<1>();
         __syncwarp();
-        const unsigned char *ks = mine + stage * (C::WARP / 2), *vs = ks + C::K_BYTES;
+        const unsigned char *ks = mine + stage * C::STAGE, *vs = ks + C::K_BYTES;
         uint32_t vals[DPL][8];
         if (cur.moved) {
             uint4 rows[DPL][2];
@@ -144,8 +147,17 @@ __global__ void __launch_bounds__(CP_WARPS * 32) compact_kernel(const CompactArg
             if (cur.moved == 0xffffu) {
 #pragma unroll
                 for (int d = 0; d < DPL; ++d) {
-                    *reinterpret_cast<uint4 *>(vd + d * 512) = make_uint4(vals[d][0], vals[d][1], vals[d][2], vals[d][3]);
-                    *reinterpret_cast<uint4 *>(vd + d * 512 + 8) = make_uint4(vals[d][4], vals[d][5], vals[d][6], vals[d][7]);
+                    // a lane pair swaps halves, so that each store writes whole 32-byte rows: first the even lane's, then the odd one's
+                    uint32_t *v = vals[d];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t give = lane & 1 ? v[i] : v[4 + i], got = __shfl_xor_sync(0xffffffffu, give, 1);
+                        if (lane & 1) v[i] = got;
+                        else v[4 + i] = got;
+                    }
+                    bf16 *even = vd - (lane & 1) * 16 + (lane & 1) * 8 + d * 512;
+                    *reinterpret_cast<uint4 *>(even) = make_uint4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<uint4 *>(even + 16) = make_uint4(v[4], v[5], v[6], v[7]);
                 }
             } else {
 #pragma unroll
@@ -327,14 +339,22 @@ extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *c
     if (x->src_stride < 0 || x->dst_stride < 0 || x->pos_stride < 0) return DEL_EINVAL;
     a.c = *x;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    // a warp for each destination page of a round: positions of up to max_count / 16 + 1 pages
-    const dim3 grid(a.kv.L * a.kv.nkv, x->batch);
-    const int warps = (x->max_count + 14) / 16 + 1 < CP_WARPS ? (x->max_count + 14) / 16 + 1 : CP_WARPS;
+    // a warp for each destination page of a round; positions of up to max_count / 16 + 2 pages
+    const int n_sms = current_sms(), pages = (x->max_count + 14) / 16 + 1, warps = pages < CP_WARPS ? pages : CP_WARPS;
+    if (!n_sms) return DEL_ECUDA;
+    const int64_t units = (int64_t)a.kv.L * a.kv.nkv * x->batch, rounds = (pages + warps - 1) / warps;
+    int64_t parts = 1;
+    if (x->src_table != x->dst_table) {
+        parts = (6 * n_sms + units - 1) / units;
+        parts = parts < rounds ? parts : rounds;
+    }
+    a.stages = (pages + parts - 1) / parts <= warps ? 1 : 2;
+    const dim3 grid(a.kv.L * a.kv.nkv, x->batch, (unsigned)parts);
     static SmemAttrOnce attr128, attr64;
-    if ((a.kv.hd == 128 ? attr128.set(compact_kernel<128>, CP_WARPS * Compact<128>::WARP) : attr64.set(compact_kernel<64>, CP_WARPS * Compact<64>::WARP)) != cudaSuccess)
+    if ((a.kv.hd == 128 ? attr128.set(compact_kernel<128>, 2 * CP_WARPS * Compact<128>::STAGE) : attr64.set(compact_kernel<64>, 2 * CP_WARPS * Compact<64>::STAGE)) != cudaSuccess)
         return DEL_ECUDA;
-    if (a.kv.hd == 128) compact_kernel<128><<<grid, warps * 32, warps * Compact<128>::WARP, st>>>(a);
-    else compact_kernel<64><<<grid, warps * 32, warps * Compact<64>::WARP, st>>>(a);
+    if (a.kv.hd == 128) compact_kernel<128><<<grid, warps * 32, a.stages * warps * Compact<128>::STAGE, st>>>(a);
+    else compact_kernel<64><<<grid, warps * 32, a.stages * warps * Compact<64>::STAGE, st>>>(a);
     return cudaGetLastError() == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }
 
