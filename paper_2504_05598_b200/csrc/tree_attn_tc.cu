@@ -140,6 +140,27 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     const int group = a.nh / a.kv.nkv;
     const int n_rt = (a.max_nodes * group + TILES * BQ - 1) / (TILES * BQ);
     const int kvh = blockIdx.y / n_rt, row0 = (blockIdx.y - kvh * n_rt) * TILES * BQ;
+    const float inv_group = 1.f / (float)group;
+    auto node_of = [&](int rr) { return (int)(((float)rr + 0.5f) * inv_group); };              // rr / group: rr < 2^16, off by less than 1/2 / group
+    auto q_row = [&](int rr) {                                      // query row rr (node x head of the group), which exists whatever nodes[b] is
+        const int i = node_of(rr);
+        return a.q + b * a.q_seq + i * a.q_node + (size_t)(kvh * group + rr - i * group) * HD;
+    };
+    // The queries are the first thing requested, before it is known how many nodes there are: 16-byte pieces, a thread every 128th
+    // of its tile.  (Each thread its own row, after the lengths: the first scores came 2.6 us into the kernel, now 1.4.)
+    constexpr int PPR = HD / 8, QP = BQ * PPR / 128;                // pieces per row, per thread
+    const int t_of = warp < 2 ? 0 : (warp - 2) >> 2, t_tid = threadIdx.x - 64 - t_of * 128;
+    uint4 q_pre[QP];
+    if (warp >= 2) {
+#pragma unroll
+        for (int e = 0; e < QP; ++e) {
+            const int u = e * 128 + t_tid, rr = row0 + t_of * BQ + u / PPR;
+            q_pre[e] = rr < a.max_nodes * group ? *reinterpret_cast<const uint4 *>(q_row(rr) + u % PPR * 8) : make_uint4(0, 0, 0, 0);
+        }
+    } else if (warp == 0 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
+    }
     const tree::Seq s = tree::load_seq(a, b);
     const int R = s.n * group;
     if (row0 >= R) return;                                          // (the whole cluster)
@@ -154,7 +175,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     const int n_warps = quarters(0) + (TILES == 2 ? quarters(TILES - 1) : 0);                  // softmax warps at work
     auto part_ml = [&](unsigned char *p, int x) { return reinterpret_cast<float2 *>(p + x * 8); };       // where the queries were
     if (threadIdx.x == 0) {
-        mbar_init(&q_full, n_warps);
+        mbar_init(&q_full, 4 * TILES);
         mbar_init(&all_bar, n_warps);
         mbar_init(&tile_bar, quarters(0));
         for (int i = 0; i < C::KS; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
@@ -173,19 +194,19 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_s)), "r"(C::TMEM) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    // Page ids (warp 0): lane i holds page i of the current four blocks, the next four are requested one round ahead.  A position
+    // behind the last, or an id that names no page, is copied from coordinate -1: zeros.
+    auto page_of = [&](int pi) {
+        const int pg = pi < n_pages ? s.pt[pi] : -1;
+        return a.kv.holds(pg) ? pg : -1;
+    };
+    int cur = warp == 0 ? page_of(PAGES * kb0 + lane) : -1, nxt = warp == 0 ? page_of(PAGES * kb0 + 32 + lane) : -1;
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = tmem_base_s;
 
     if (warp == 0) {
-        // Page ids: lane i holds page i of the current four blocks, the next four are requested one round ahead.  A position
-        // behind the last, or an id that names no page, is copied from coordinate -1: zeros.
-        auto page_of = [&](int pi) {
-            const int pg = pi < n_pages ? s.pt[pi] : -1;
-            return a.kv.holds(pg) ? pg : -1;
-        };
-        int cur = page_of(PAGES * kb0 + lane), nxt = page_of(PAGES * kb0 + 32 + lane);
         int n_k = 0, n_v = 0;                        // blocks whose keys, whose values are on their way
         for (int j = 0; j < n_kb; ++j) {
             const int ks = j % C::KS, vs = j % C::VS, first = (PAGES * j) & 31;
@@ -286,20 +307,19 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
         const int t = (warp - 2) >> 2, q = warp & 3;             // tile, TMEM lane quarter this warp may access
         const int trow = q * 32 + lane, rr = row0 + t * BQ + trow, nq = quarters(t);
         const bool row_ok = rr < R;
+        // queries: rows of 128-byte k-blocks with the 128-byte swizzle
+#pragma unroll
+        for (int e = 0; e < QP; ++e) {
+            const int u = e * 128 + t_tid, r = u / PPR, c = u % PPR;
+            *reinterpret_cast<uint4 *>(q_sm + t * C::KB * C::Q_PART + (c >> 3) * C::Q_PART + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = q_pre[e];
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&q_full);
         if (q < nq) {
-            // queries: row of 128-byte k-blocks with the 128-byte swizzle; rows behind the last are zero
-            const int i = row_ok ? rr / group : 0, hq = row_ok ? rr - i * group : 0;
+            const int i = row_ok ? node_of(rr) : 0, hq = row_ok ? rr - i * group : 0;
             const uint64_t bits = row_ok ? tree::node_bits(a, b, i) : 0;
             const bf16 *qp = a.q + b * a.q_seq + i * a.q_node + (size_t)(kvh * group + hq) * HD;
-            unsigned char *qrow = q_sm + t * C::KB * C::Q_PART + trow * 128;
-#pragma unroll
-            for (int c = 0; c < HD / 8; ++c) {
-                const uint4 v = row_ok ? *reinterpret_cast<const uint4 *>(qp + 8 * c) : make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(qrow + (c >> 3) * C::Q_PART + (((c & 7) ^ (trow & 7)) << 4)) = v;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&q_full);
             // does the table name pages that are none?  (then every block's ids are looked at again)
             bool bad = false;
             for (int p = PAGES * kb0 + trow; p < min(n_pages, PAGES * (kb0 + n_kb)); p += nq * 32) bad |= !a.kv.holds(s.pt[p]);
@@ -409,7 +429,8 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     unsigned char *vst = v_sm + (j % C::VS) * C::V_BYTES;
                     if (!wait_or_err(&v_full[j % C::VS], (j / C::VS) & 1, &s_err)) { if (!s_err) s_err = 10; ok = false; break; }
                     bool odd = false;
-                    for (int u = trow; u < PAGES * HD * 2; u += nq * 32) {
+                    const int u0 = max(0, (s.len - key0) >> 4) * HD * 2, u1 = min(PAGES, n_pages - (key0 >> 4)) * HD * 2;     // (pages behind the last are zeros)
+                    for (int u = u0 + trow; u < u1; u += nq * 32) {
                         const uint4 v = *reinterpret_cast<const uint4 *>(vst + u * 16);
                         odd |= odd_pair(v.x) | odd_pair(v.y) | odd_pair(v.z) | odd_pair(v.w);
                     }
@@ -494,31 +515,49 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     if (n_splits > 1) {
         cg::cluster_group cl = cg::this_cluster();
         cl.sync();
-        // the parts' states of one row each: a warp takes a row of the cluster's rows, every lane four columns
-        bool failed = false;
-        for (int k = 0; k < n_splits; ++k) failed |= *cl.map_shared_rank(const_cast<int *>(&s_err), k) != 0;
-        constexpr int LPR = HD / 4;                                 // lanes per row
-        for (int x = (split * C::THREADS + threadIdx.x) / LPR; x < rows; x += n_splits * C::THREADS / LPR) {
-            const int c = threadIdx.x % LPR;
-            float M = -INFINITY;
-            for (int k = 0; k < n_splits; ++k) M = fmaxf(M, part_ml(cl.map_shared_rank(q_sm, k), x)->x);
-            const float mu = M == -INFINITY ? 0.f : M;
-            float L = 0.f;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < n_splits; ++k) {
-                const float2 ml = *part_ml(cl.map_shared_rank(q_sm, k), x);
-                if (k * per >= nb) break;                           // (this part and the later ones have no block)
-                const float w = ex2f(ml.x - mu);
-                const float4 v = *reinterpret_cast<const float4 *>(cl.map_shared_rank(reinterpret_cast<float *>(k_sm), k) + (size_t)x * HD + ((c ^ (x & 15)) << 2));
-                L += ml.y * w;
-                o.x += v.x * w; o.y += v.y * w; o.z += v.z * w; o.w += v.w * w;
+        // Each CTA finishes a share of the rows: first the parts' weights, a thread per row; then the outputs, four columns per thread,
+        // all parts' loads on their way together.
+        constexpr int LPR = HD / 4, MAX_PARTS = 8;
+        const int parts = (nb + per - 1) / per, mine0 = rows * split / n_splits, mine1 = rows * (split + 1) / n_splits;     // (parts with blocks, this CTA's rows)
+        float *w_sm = reinterpret_cast<float *>(q_sm + TILES * BQ * 8);                          // [row][MAX_PARTS]
+        for (int x = mine0 + threadIdx.x; x < mine1; x += C::THREADS) {
+            float2 ml[MAX_PARTS];
+            bool failed = false;
+#pragma unroll
+            for (int k = 0; k < MAX_PARTS; ++k) {
+                ml[k] = k < parts ? *part_ml(cl.map_shared_rank(q_sm, k), x) : make_float2(-INFINITY, 0.f);
+                failed |= k < n_splits && *cl.map_shared_rank(const_cast<int *>(&s_err), k) != 0;
             }
+            float M = -INFINITY, L = 0.f;
+#pragma unroll
+            for (int k = 0; k < MAX_PARTS; ++k) M = fmaxf(M, ml[k].x);
+            const float mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+            for (int k = 0; k < MAX_PARTS; ++k) { ml[k].x = ex2f(ml[k].x - mu); L += ml[k].y * ml[k].x; }
             const float inv = failed ? NAN : L == 0.f ? 0.f : 1.f / L;
-            const int rr = row0 + x, i = rr / group, hq = rr - i * group;
+#pragma unroll
+            for (int k = 0; k < MAX_PARTS; ++k) w_sm[x * MAX_PARTS + k] = ml[k].x * inv;
+        }
+        __syncthreads();
+        for (int e = mine0 * LPR + threadIdx.x; e < mine1 * LPR; e += C::THREADS) {
+            const int x = e / LPR, c = e % LPR;
+            const size_t off = (size_t)x * HD + ((c ^ (x & 15)) << 2);
+            float4 v[MAX_PARTS];
+#pragma unroll
+            for (int k = 0; k < MAX_PARTS; ++k)
+                if (k < parts) v[k] = *reinterpret_cast<const float4 *>(cl.map_shared_rank(reinterpret_cast<float *>(k_sm), k) + off);
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < MAX_PARTS; ++k)
+                if (k < parts) {
+                    const float w = w_sm[x * MAX_PARTS + k];
+                    o.x += v[k].x * w; o.y += v[k].y * w; o.z += v[k].z * w; o.w += v[k].w * w;
+                }
+            const int rr = row0 + x, i = node_of(rr), hq = rr - i * group;
             const size_t at = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD + 4 * c;
             uint2 hi, lo;
-            split_bf16x2(o.x * inv, o.y * inv, hi.x, lo.x);
-            split_bf16x2(o.z * inv, o.w * inv, hi.y, lo.y);
+            split_bf16x2(o.x, o.y, hi.x, lo.x);
+            split_bf16x2(o.z, o.w, hi.y, lo.y);
             *reinterpret_cast<uint2 *>(a.out + at) = hi;
             if (a.out_lo) *reinterpret_cast<uint2 *>(a.out_lo + at) = lo;
         }
