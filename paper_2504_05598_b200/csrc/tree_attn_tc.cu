@@ -6,13 +6,13 @@
 // pages [16][hd] and the value pages [hd][16] are the K-major operand tiles tcgen05.mma wants, so TMA copies them as they lie (5-d maps
 // of the cache, 128-byte swizzle for keys, 32-byte swizzle for values).  Per block and tile:
 //   S = Q K^T      M 128, N 128, into tensor memory;
-//   softmax        one thread per query row, two sweeps of tcgen05.ld over its 128 scores: their maximum; then p = 2^(s - m) against a
-//                  lazily raised reference m (the output in tensor memory is rescaled only when the row maximum has grown by more
-//                  than 2^8), written as bf16 over the scores;
+//   softmax        two threads per query row, in two warps, 64 scores each: two sweeps of tcgen05.ld, first their maximum, exchanged through
+//                  shared memory; then p = 2^(s - m) against a lazily raised reference m (the output in tensor memory is rescaled
+//                  only when the row maximum has grown by more than 2^8), written as bf16 over the scores;
 //   O += P V       M 128, N hd, K 16 per page, P read from tensor memory.
 // Shared memory's 128 bytes per clock are what the MMAs compete for: with N = 64 and P in shared memory, scores and products of a
 // block of 64 keys read 80 KB per tile (640 cycles, 256 of arithmetic); with N = 128 and P in tensor memory 48 KB.
-// Roles: warp 0 issues the copies, warp 1 the MMAs, four warps per tile do the softmax; quarters of a tile without rows do nothing.
+// Roles: warp 0 issues the copies, warp 1 the MMAs, eight warps per tile do the softmax; quarters of a tile without rows do nothing.
 // With two tiles each has one score buffer and one tile's softmax runs beside the other's MMAs; a single tile has two buffers.
 // Every mbarrier wait is bounded and gives up as soon as another role has: the rows then become NaN and the caller's error word, if
 // there is one, is set.
@@ -42,17 +42,17 @@ struct Cfg {
     static constexpr int Q_PART = BQ * 128;                        // [128 rows][128 B]
     static constexpr int Q_BYTES = TILES * KB * Q_PART;
     static constexpr int K_BYTES = KB * BKEY * 128, V_BYTES = PAGES * HD * 32;
-    static constexpr int KS = HD == 128 ? (TILES == 2 ? 2 : 3) : 5, VS = HD == 128 ? 3 : 6;      // blocks in the rings
+    static constexpr int KS = HD == 128 ? (TILES == 2 ? 2 : 3) : 5, VS = HD == 128 ? 2 : 5;      // blocks in the rings
     static constexpr int RING = KS * K_BYTES + VS * V_BYTES;
     static constexpr int O_BYTES = TILES * BQ * HD * 4;            // the parts' outputs, where the rings were
     static constexpr int SMEM = Q_BYTES + RING + 1024;
-    static constexpr int THREADS = 64 + TILES * 128;
+    static constexpr int THREADS = 64 + TILES * 256;
     static constexpr int BUFS = 2;                                 // score buffers: one per tile, or two of the only tile
     static constexpr uint32_t O_COL = BUFS * BKEY;                 // score buffers first, then the outputs
     static constexpr uint32_t TMEM = 512;
     static_assert(O_BYTES <= RING, "outputs do not fit where the rings were");
     static_assert(O_COL + TILES * HD <= TMEM, "too much tensor memory");
-    static_assert(SMEM <= 232448 - 512, "too much shared memory");
+    static_assert(SMEM <= 232448 - 3072, "too much shared memory");
 };
 
 struct Maps { CUtensorMap k, v; };
@@ -127,10 +127,11 @@ template <int HD, int TILES>
 __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TreeArgs a) {
     using C = Cfg<HD, TILES>;
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) uint64_t q_full, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], s_full[2], p_full[2], o_done[TILES], tile_bar, all_bar;
+    __shared__ __align__(8) uint64_t q_full, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], s_full[2], p_full[2], o_done[TILES], tile_bar, all_bar, pair_bar[TILES][4];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile int s_err;
     __shared__ int s_bad_page, s_odd[2];
+    __shared__ float s_max[2][2][BQ], s_sum[TILES][BQ];             // [tile, or buffer of the only one][half][row] block maxima; the second halves' sums
     __shared__ unsigned long long s_odd_tokens;                     // drafted tokens whose values were zeroed
     unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~(uintptr_t)1023);
     unsigned char *q_sm = base, *k_sm = base + C::Q_BYTES, *v_sm = k_sm + C::KS * C::K_BYTES;
@@ -146,15 +147,15 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
         const int i = node_of(rr);
         return a.q + b * a.q_seq + i * a.q_node + (size_t)(kvh * group + rr - i * group) * HD;
     };
-    // The queries are the first thing requested, before it is known how many nodes there are: 16-byte pieces, a thread every 128th
+    // The queries are the first thing requested, before it is known how many nodes there are: 16-byte pieces, a thread every 256th
     // of its tile.  (Each thread its own row, after the lengths: the first scores came 2.6 us into the kernel, now 1.4.)
-    constexpr int PPR = HD / 8, QP = BQ * PPR / 128;                // pieces per row, per thread
-    const int t_of = warp < 2 ? 0 : (warp - 2) >> 2, t_tid = threadIdx.x - 64 - t_of * 128;
+    constexpr int PPR = HD / 8, QP = BQ * PPR / 256;                // pieces per row, per thread
+    const int t_of = warp < 2 ? 0 : (warp - 2) >> 3, t_tid = threadIdx.x - 64 - t_of * 256;
     uint4 q_pre[QP];
     if (warp >= 2) {
 #pragma unroll
         for (int e = 0; e < QP; ++e) {
-            const int u = e * 128 + t_tid, rr = row0 + t_of * BQ + u / PPR;
+            const int u = e * 256 + t_tid, rr = row0 + t_of * BQ + u / PPR;
             q_pre[e] = rr < a.max_nodes * group ? *reinterpret_cast<const uint4 *>(q_row(rr) + u % PPR * 8) : make_uint4(0, 0, 0, 0);
         }
     } else if (warp == 0 && lane == 0) {
@@ -172,17 +173,19 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
 
     auto quarters = [&](int t) { return min(4, max(0, (R - row0 - t * BQ + 31) >> 5)); };      // of tile t, that have rows
     const int n_tiles = TILES == 2 && quarters(1) > 0 ? 2 : 1;
-    const int n_warps = quarters(0) + (TILES == 2 ? quarters(TILES - 1) : 0);                  // softmax warps at work
+    const int n_warps = 2 * (quarters(0) + (TILES == 2 ? quarters(TILES - 1) : 0));            // softmax warps at work
     auto part_ml = [&](unsigned char *p, int x) { return reinterpret_cast<float2 *>(p + x * 8); };       // where the queries were
     if (threadIdx.x == 0) {
-        mbar_init(&q_full, 4 * TILES);
+        mbar_init(&q_full, 8 * TILES);
         mbar_init(&all_bar, n_warps);
-        mbar_init(&tile_bar, quarters(0));
+        mbar_init(&tile_bar, 2 * quarters(0));
+        for (int t = 0; t < TILES; ++t)
+            for (int i = 0; i < 4; ++i) mbar_init(&pair_bar[t][i], 2);
         for (int i = 0; i < C::KS; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
         for (int i = 0; i < C::VS; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&s_full[i], 1);
-            mbar_init(&p_full[i], TILES == 2 ? max(1, quarters(i)) : quarters(0));
+            mbar_init(&p_full[i], 2 * (TILES == 2 ? max(1, quarters(i)) : quarters(0)));
         }
         for (int t = 0; t < TILES; ++t) mbar_init(&o_done[t], 1);
         s_err = 0;
@@ -275,7 +278,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                 for (int kk = 0; kk < PAGES; ++kk)
-                    umma_bf16_ts(tmem_base + C::O_COL + (uint32_t)(t * HD), tmem_base + (uint32_t)(buf * BKEY + kk * 8),
+                    umma_bf16_ts(tmem_base + C::O_COL + (uint32_t)(t * HD), tmem_base + (uint32_t)(buf * BKEY + (kk >> 2) * 64 + (kk & 3) * 8),
                                  umma_desc_sw32(v_addr + (j % C::VS) * C::V_BYTES + kk * HD * 32), idesc_o, (j | kk) != 0);
                 umma_commit(&o_done[t]);
                 ++n_p[t];
@@ -304,13 +307,13 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             }
         }
     } else {
-        const int t = (warp - 2) >> 2, q = warp & 3;             // tile, TMEM lane quarter this warp may access
+        const int t = t_of, half = ((warp - 2) >> 2) & 1, q = warp & 3;      // tile, which 64 of a block's keys, TMEM lane quarter this warp may access
         const int trow = q * 32 + lane, rr = row0 + t * BQ + trow, nq = quarters(t);
         const bool row_ok = rr < R;
         // queries: rows of 128-byte k-blocks with the 128-byte swizzle
 #pragma unroll
         for (int e = 0; e < QP; ++e) {
-            const int u = e * 128 + t_tid, r = u / PPR, c = u % PPR;
+            const int u = e * 256 + t_tid, r = u / PPR, c = u % PPR;
             *reinterpret_cast<uint4 *>(q_sm + t * C::KB * C::Q_PART + (c >> 3) * C::Q_PART + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = q_pre[e];
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             const bf16 *qp = a.q + b * a.q_seq + i * a.q_node + (size_t)(kvh * group + hq) * HD;
             // does the table name pages that are none?  (then every block's ids are looked at again)
             bool bad = false;
-            for (int p = PAGES * kb0 + trow; p < min(n_pages, PAGES * (kb0 + n_kb)); p += nq * 32) bad |= !a.kv.holds(s.pt[p]);
+            for (int p = PAGES * kb0 + half * nq * 32 + trow; p < min(n_pages, PAGES * (kb0 + n_kb)); p += 2 * nq * 32) bad |= !a.kv.holds(s.pt[p]);
             if (__any_sync(0xffffffffu, bad) && lane == 0) s_bad_page = 1;
             // barriers among softmax warps, bounded like every wait
             auto meet = [&](uint64_t *bar, uint32_t parity) -> bool {
@@ -339,42 +342,40 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             const uint32_t o_addr = lane_addr + C::O_COL + (uint32_t)(t * HD);
             float m_ref = -INFINITY, l = 0.f;
             for (int j = 0; ok && j < n_kb; ++j) {
-                const int buf = TILES == 2 ? t : j & 1, key0 = (kb0 + j) * BKEY;
-                const uint32_t s_addr = lane_addr + (uint32_t)(buf * BKEY);
+                const int buf = TILES == 2 ? t : j & 1, key0 = (kb0 + j) * BKEY, key1 = key0 + 64 * half;
+                const uint32_t s_addr = lane_addr + (uint32_t)(buf * BKEY + 64 * half);
                 const bool tail = key0 + BKEY > s.len, masked = tail || bad_pages;
-                uint64_t vm[2] = {~0ull, ~0ull};
+                uint64_t vm = ~0ull;
                 if (masked) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        vm[h] = visible(bits, key0 + 64 * h, s.len, s.n_keys);
-                        for (int pg = 0; bad_pages && pg < 4; ++pg) {
-                            const int pi = (key0 >> 4) + 4 * h + pg;
-                            if (pi >= n_pages || !a.kv.holds(s.pt[pi])) vm[h] &= ~(0xffffull << (16 * pg));
-                        }
+                    vm = visible(bits, key1, s.len, s.n_keys);
+                    for (int pg = 0; bad_pages && pg < 4; ++pg) {
+                        const int pi = (key1 >> 4) + pg;
+                        if (pi >= n_pages || !a.kv.holds(s.pt[pi])) vm &= ~(0xffffull << (16 * pg));
                     }
                 }
                 if (!wait_or_err(&s_full[buf], (TILES == 2 ? j : j >> 1) & 1, &s_err)) { if (!s_err) s_err = 8; ok = false; break; }
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                uint32_t r[2][32];
-                auto mask_chunk = [&](uint32_t (&x)[32], int c) {
-                    const uint32_t v = (uint32_t)(vm[c >> 1] >> (32 * (c & 1)));
+                uint32_t x[32];
+                auto mask_chunk = [&](int c) {
+                    const uint32_t v = (uint32_t)(vm >> (32 * c));
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         if (!((v >> e) & 1)) x[e] = 0xff800000u;
                 };
-                // first sweep: the maximum
+                // first sweep: the maximum, of both halves
                 float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                tmem_ld32(s_addr, r[0]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 1; c >= 0; --c) {                    // (the first chunk last: the second sweep begins with it)
+                    tmem_ld32(s_addr + 32 * c, x);
                     tmem_ld_wait();
-                    if (c < 3) tmem_ld32(s_addr + 32 * (c + 1), r[(c + 1) & 1]);
-                    else tmem_ld32(s_addr, r[0]);                 // (the second sweep's first)
-                    if (masked) mask_chunk(r[c & 1], c);
+                    if (masked) mask_chunk(c);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(r[c & 1][e]));
+                    for (int e = 0; e < 32; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(x[e]));
                 }
-                const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * a.scale;
+                float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                s_max[buf][half][trow] = mx;
+                if (!meet(&pair_bar[t][q], j & 1)) { if (!s_err) s_err = 14; ok = false; break; }
+                mx = fmaxf(mx, s_max[buf][half ^ 1][trow]) * a.scale;
                 // reference maximum: raised only when the row maximum has outgrown it by RESCALE_STEP
                 float alpha = 1.f;
                 if (m_ref == -INFINITY) {
@@ -385,27 +386,29 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     l *= alpha;
                 }
                 const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-                // second sweep: probabilities, as bf16 over the scores that have been read
+                // second sweep: probabilities, as bf16 over the scores of this half that have been read
                 float ps[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    tmem_ld_wait();
-                    uint32_t (&x)[32] = r[c & 1];
-                    if (c < 3) tmem_ld32(s_addr + 32 * (c + 1), r[(c + 1) & 1]);
-                    if (masked) mask_chunk(x, c);
-                    float f[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(x[e]);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) fma2(f[e], f[e + 1], a.scale, -m_use);
+                for (int c = 0; c < 2; ++c) {
+                    if (c == 1) {
+                        tmem_ld32(s_addr + 32, x);
+                        tmem_ld_wait();
+                        if (masked) mask_chunk(1);
+                    }
                     uint32_t pk[16];
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
-                        f[e] = ex2f(f[e]); f[e + 1] = ex2f(f[e + 1]); f[e + 2] = ex2f(f[e + 2]); f[e + 3] = ex2f(f[e + 3]);
-                        add2(ps[0], ps[1], f[e], f[e + 1]);
-                        add2(ps[2], ps[3], f[e + 2], f[e + 3]);
-                        pk[e / 2] = pack_bf16(f[e], f[e + 1]);
-                        pk[e / 2 + 1] = pack_bf16(f[e + 2], f[e + 3]);
+                        float f[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(x[e + i]);
+                        fma2(f[0], f[1], a.scale, -m_use);
+                        fma2(f[2], f[3], a.scale, -m_use);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) f[i] = ex2f(f[i]);
+                        add2(ps[0], ps[1], f[0], f[1]);
+                        add2(ps[2], ps[3], f[2], f[3]);
+                        pk[e / 2] = pack_bf16(f[0], f[1]);
+                        pk[e / 2 + 1] = pack_bf16(f[2], f[3]);
                     }
                     tmem_st16(s_addr + 16 * c, pk);
                 }
@@ -414,13 +417,12 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     // (the previous block's products are part of the output; with one tile they may still be running)
                     if (TILES == 1 && !wait_or_err(&o_done[t], (j - 1) & 1, &s_err)) { if (!s_err) s_err = 9; ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    for (int c0 = 0; c0 < HD; c0 += 32) {
-                        uint32_t o[32];
-                        tmem_ld32(o_addr + (uint32_t)c0, o);
+                    for (int c0 = half * (HD / 2); c0 < (half + 1) * (HD / 2); c0 += 32) {
+                        tmem_ld32(o_addr + (uint32_t)c0, x);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                        tmem_st32(o_addr + (uint32_t)c0, o);
+                        for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * alpha);
+                        tmem_st32(o_addr + (uint32_t)c0, x);
                     }
                 }
                 if (tail && t == 0) {
@@ -430,14 +432,14 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     if (!wait_or_err(&v_full[j % C::VS], (j / C::VS) & 1, &s_err)) { if (!s_err) s_err = 10; ok = false; break; }
                     bool odd = false;
                     const int u0 = max(0, (s.len - key0) >> 4) * HD * 2, u1 = min(PAGES, n_pages - (key0 >> 4)) * HD * 2;     // (pages behind the last are zeros)
-                    for (int u = u0 + trow; u < u1; u += nq * 32) {
+                    for (int u = u0 + half * nq * 32 + trow; u < u1; u += 2 * nq * 32) {
                         const uint4 v = *reinterpret_cast<const uint4 *>(vst + u * 16);
                         odd |= odd_pair(v.x) | odd_pair(v.y) | odd_pair(v.z) | odd_pair(v.w);
                     }
                     if (__any_sync(0xffffffffu, odd) && lane == 0) s_odd[j & 1] = 1;      // (never cleared: two blocks later it only costs time)
                     if (!meet(&tile_bar, tile_phase)) { if (!s_err) s_err = 11; ok = false; break; }
                     tile_phase ^= 1;
-                    for (int e = q; s_odd[j & 1] && e < BKEY; e += nq) {
+                    for (int e = 2 * q + half; s_odd[j & 1] && e < BKEY; e += 2 * nq) {
                         if (key0 + e < s.len) continue;           // committed: every row sees it
                         const int tk = e & 15;
                         unsigned char *col = vst + (e >> 4) * HD * 32 + (tk & 7) * 2;
@@ -456,16 +458,23 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                 if (lane == 0) mbar_arrive(&p_full[buf]);
             }
             if (ok && n_kb > 0 && !wait_or_err(&o_done[t], (n_kb - 1) & 1, &s_err)) { if (!s_err) s_err = 12; ok = false; }
-            if (!meet(&all_bar, 1)) { if (!s_err) s_err = 13; ok = false; }       // both tiles are done with the rings, s_odd_tokens is complete
+            if (half) s_sum[t][trow] = l;
+            if (!meet(&all_bar, 1)) { if (!s_err) s_err = 13; ok = false; }       // both tiles are done with the rings, s_odd_tokens and the sums are complete
+            l = half ? l : l + s_sum[t][trow];                   // (the first half's threads go on with the sum)
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint64_t odd_seen = s_odd_tokens & bits;
             const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
             const size_t head = ((size_t)(a.layer - 1) * a.kv.nkv + kvh) * a.kv.head_elems();
+            if (n_splits == 1) {                                   // (then the second half's need it as well)
+                if (!half) s_sum[t][trow] = l;
+                if (!meet(&pair_bar[t][q], n_kb & 1)) { if (!s_err) s_err = 15; ok = false; }
+                l = s_sum[t][trow];
+            }
             const float inv = l == 0.f ? 0.f : 1.f / l;            // (l = 0: nothing is visible, the result is zero)
             const size_t out = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD;
-            if (n_splits > 1) *part_ml(q_sm, t * BQ + trow) = make_float2(m_ref, l);
+            if (n_splits > 1 && !half) *part_ml(q_sm, t * BQ + trow) = make_float2(m_ref, l);
             float *po = reinterpret_cast<float *>(k_sm) + (size_t)(t * BQ + trow) * HD;
-            for (int c0 = 0; c0 < HD && n_kb > 0; c0 += 32) {
+            for (int c0 = half * (HD / 2); c0 < (half + 1) * (HD / 2) && n_kb > 0; c0 += 32) {
                 uint32_t o[32];
                 if (ok) tmem_ld32(o_addr + (uint32_t)c0, o);
                 tmem_ld_wait();
