@@ -352,7 +352,7 @@ typedef struct {
     const uint64_t *mask;         /* [batch][max_nodes], may be null: a chain, node i sees nodes 0..i */
     int32_t *error;               /* may be null; else set to a non-zero code if a bounded device-side wait expired: the rows concerned are NaN */
     int64_t q_seq_stride, q_node_stride, out_seq_stride, out_node_stride;   /* in elements, multiples of 8 */
-    int32_t batch, max_nodes, n_heads;       /* max_nodes 1..64, n_heads a multiple of n_kv_heads, batch 1..65535 */
+    int32_t batch, max_nodes, n_heads;       /* max_nodes 1..64, n_heads a multiple (up to 1024) of n_kv_heads, batch 1..65535 */
     int32_t layer;                /* 1-based */
     int32_t table_cols, table_stride;
     int32_t max_len;              /* what lens are expected to reach (0: table_cols * 16): splits the work, changes no result but for the order of sums */

@@ -50,3 +50,36 @@ inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, i
     cfg.numAttrs = cluster_x > 1 ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
+
+// How many clusters of `cluster_x` CTAs of a kernel the current device keeps resident, asked once per device and size (sizes 1..16,
+// `kept`: the caller's record per kernel).  A launch of more runs in waves: of clusters of 8 with one CTA per SM, B200 holds 15.
+struct ClusterRoom {
+    int n[DEL_MAX_DEVICES][17] = {};
+    template <typename K> int of(K kern, int threads, size_t smem, int cluster_x) {
+        int dev = 0;
+        if (cluster_x < 1 || cluster_x > 16 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEL_MAX_DEVICES) return 0;
+        if (n[dev][cluster_x]) return n[dev][cluster_x];
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(cluster_x);
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = cluster_x;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        int got = 0;
+        if (cudaOccupancyMaxActiveClusters(&got, kern, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            return 0;
+        }
+        return n[dev][cluster_x] = got;
+    }
+    // the largest cluster size up to `most` (1: none) of which `units` are resident together
+    template <typename K> int best(K kern, int threads, size_t smem, int64_t units, int most) {
+        for (int c = most < 8 ? most : 8; c > 1; --c)
+            if (units <= of(kern, threads, smem, c)) return c;
+        return 1;
+    }
+};

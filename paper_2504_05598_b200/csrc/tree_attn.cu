@@ -1,7 +1,7 @@
 // Attention of a tree of drafted tokens over the paged cache (del_tree_attention).
 //
 // For every sequence, kv head and tile of 16 query rows (node x query head of the group) one cluster of CTAs walks the pages of
-// the key range, each CTA a contiguous part of it and each of its warps every eighth page.  A warp keeps the online-softmax state of
+// the keys, each warp of it every so manyth page (so that the first page ids can be requested before the lengths are known).  A warp keeps the online-softmax state of
 // the tile in registers: S = Q K^T and O += P V are bf16 m16n8k16 MMAs with fp32 sums, the running maximum and sum are fp32.  The warps
 // join through shared memory, the CTAs of the cluster through distributed shared memory: one launch, no workspace, a fixed order
 // of sums.
@@ -24,11 +24,12 @@ namespace {
 
 using namespace tree;
 
-constexpr int NW = 8, THREADS = NW * 32, MAX_SPLITS = 16;
+constexpr int NW = 8, THREADS = NW * 32;
+static_assert(NW == 8, "the join of the warps adds four pairs");
 constexpr float LOG2E = 1.4426950408889634f;
 
 template <int HD>
-__global__ void __launch_bounds__(THREADS) tree_attention_kernel(const TreeArgs a) {
+__global__ void __launch_bounds__(THREADS, HD == 64 ? 2 : 1) tree_attention_kernel(const TreeArgs a) {
     constexpr int KS = HD / 32, NJ = HD / 8, LD = HD + 8;
     __shared__ float so[NW / 2][16][LD];
     __shared__ float2 sml[NW][16];
@@ -37,6 +38,14 @@ __global__ void __launch_bounds__(THREADS) tree_attention_kernel(const TreeArgs 
     const int n_splits = gridDim.x, split = blockIdx.x;
     const int group = a.nh / a.kv.nkv, n_mt = (a.max_nodes * group + 15) >> 4;
     const int kvh = blockIdx.y / n_mt, mt = blockIdx.y - kvh * n_mt, b = blockIdx.z;
+    // page ids: lane i holds the id of the warp's i-th page of the current 32
+    const int p_first = split * NW + warp, p_step = n_splits * NW;
+    const int32_t *pt = a.table + (size_t)b * a.stride;
+    auto ids = [&](int i0) {
+        const int64_t p = p_first + (int64_t)p_step * (i0 + lane);
+        return p < a.cols ? pt[p] : -1;
+    };
+    int id32 = ids(0);
     const Seq s = load_seq(a, b);
     const int R = s.n * group;
     if (mt * 16 >= R) return;                                   // (the whole cluster)
@@ -59,14 +68,13 @@ __global__ void __launch_bounds__(THREADS) tree_attention_kernel(const TreeArgs 
 #pragma unroll
     for (int j = 0; j < NJ; ++j) O[j][0] = O[j][1] = O[j][2] = O[j][3] = 0.f;
 
-    const int n_pages = (s.n_keys + 15) >> 4, pps = (n_pages + n_splits - 1) / n_splits;
-    const int p_begin = split * pps, p_end = min(n_pages, p_begin + pps);
+    const int n_pages = (s.n_keys + 15) >> 4;
     const size_t page_stride = a.kv.page_elems(), head_off = ((size_t)(a.layer - 1) * a.kv.nkv + kvh) * a.kv.head_elems();
     const int key0 = 4 * (g >> 1) + (g & 1);                    // token of column g of score tile 0; tile 1: +2
-
-    for (int p = p_begin + warp; p < p_end; p += NW) {
-        const int pg = s.pt[p];
-        if (!a.kv.holds(pg)) continue;
+    for (int p = p_first, it = 0; p < n_pages; p += p_step, ++it) {
+        if (it > 0 && (it & 31) == 0) id32 = ids(it);
+        const int pg = __shfl_sync(0xffffffffu, id32, it & 31);
+        if (!a.kv.holds(pg)) continue;                          // (the same in every lane)
         const bf16 *kp = a.kv.k + (size_t)pg * page_stride + head_off, *vp = a.kv.v + (size_t)pg * page_stride + head_off;
         uint4 kf[2][KS];
         uint2 vf[NJ];
@@ -226,19 +234,12 @@ __global__ void __launch_bounds__(THREADS) tree_attention_kernel(const TreeArgs 
 }
 
 template <int HD>
-cudaError_t launch(const TreeArgs &a, int batch, int splits, cudaStream_t st) {
-    auto kern = tree_attention_kernel<HD>;
-    static bool big[DEL_MAX_DEVICES] = {};
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (splits > 8 && !(dev < DEL_MAX_DEVICES && big[dev])) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        if (dev < DEL_MAX_DEVICES) big[dev] = true;
-    }
+cudaError_t launch(const TreeArgs &a, int batch, int pages, cudaStream_t st) {
+    static ClusterRoom room;
     const int group = a.nh / a.kv.nkv, n_mt = (a.max_nodes * group + 15) / 16;
-    return launch_cluster(kern, dim3(splits, a.kv.nkv * n_mt, batch), THREADS, 0, splits, st, a);
+    const int64_t units = (int64_t)a.kv.nkv * n_mt * batch;
+    const int splits = room.best(tree_attention_kernel<HD>, THREADS, 0, units, (pages + NW - 1) / NW);      // (a page per warp at least)
+    return launch_cluster(tree_attention_kernel<HD>, dim3(splits, a.kv.nkv * n_mt, batch), THREADS, 0, splits, st, a);
 }
 
 }  // namespace
@@ -252,27 +253,35 @@ extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, v
     if (((uintptr_t)x->page_table | (uintptr_t)x->lens | (uintptr_t)x->nodes | (uintptr_t)x->error) & 3 || (uintptr_t)x->mask & 7) return DEL_EINVAL;
     if ((x->q_seq_stride | x->q_node_stride | x->out_seq_stride | x->out_node_stride) & 7) return DEL_EINVAL;
     if (x->batch < 1 || x->batch > 65535 || x->max_nodes < 1 || x->max_nodes > 64) return DEL_EINVAL;
-    if (x->n_heads < 1 || x->n_heads % a.kv.nkv || x->layer < 1 || x->layer > a.kv.L) return DEL_EINVAL;
+    if (x->n_heads < 1 || x->n_heads % a.kv.nkv || x->n_heads / a.kv.nkv > 1024 || x->layer < 1 || x->layer > a.kv.L) return DEL_EINVAL;
     if (x->table_cols < 1 || x->table_cols > (INT32_MAX - 1024) / 16 || x->table_stride < 0 || x->max_len < 0) return DEL_EINVAL;
     if (!(x->scale >= 0.f && x->scale < INFINITY)) return DEL_EINVAL;
     const int64_t group = x->n_heads / a.kv.nkv, tiles = (x->max_nodes * group + 15) / 16;
     if (tiles * a.kv.nkv > 65535) return DEL_EINVAL;
-    const int n_sms = current_sms();
-    if (!n_sms) return DEL_ECUDA;
     a.q = (const bf16 *)x->q; a.out = (bf16 *)x->out; a.out_lo = (bf16 *)x->out_lo;
     a.table = x->page_table; a.lens = x->lens; a.nodes = x->nodes; a.mask = x->mask;
     a.q_seq = x->q_seq_stride; a.q_node = x->q_node_stride; a.o_seq = x->out_seq_stride; a.o_node = x->out_node_stride;
     a.max_nodes = x->max_nodes; a.nh = x->n_heads; a.layer = x->layer; a.cols = x->table_cols; a.stride = x->table_stride;
     a.scale = (x->scale > 0.f ? x->scale : 1.f / sqrtf((float)a.kv.hd)) * LOG2E;
     a.err = x->error;
-    const int64_t units = tiles * a.kv.nkv * x->batch;
     const int len = x->max_len ? (x->max_len < x->table_cols * 16 ? x->max_len : x->table_cols * 16) : x->table_cols * 16;
     const int pages = (len + x->max_nodes + 15) / 16;
-    if (x->max_nodes * group > 16)
-        return launch_tree_attention_tc(a, x->batch, len, n_sms, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
-    int splits = 1;
-    while (splits < MAX_SPLITS && units * splits * 2 <= 2 * n_sms && pages > splits * NW) splits *= 2;
-    cudaError_t e = a.kv.hd == 128 ? launch<128>(a, x->batch, splits, (cudaStream_t)cuda_stream)
-                                   : launch<64>(a, x->batch, splits, (cudaStream_t)cuda_stream);
+    // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 256 rows, but starts 2 to 3 us later.
+    // The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync / tcgen05, two kv layers in turn:
+    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions 7.8 /  9.4,  1000:  8.7 / 10.4,  4000: 14.6 / 14.4
+    //   8B shape, 4 x 8 nodes (64 tiles)     200           8.0 /  9.7,  1000: 11.2 / 12.3,  2000: 17.9 / 15.1,  4000: 27.8 /  22.1
+    //   13B shape, 1 x 26 nodes (80 tiles)   200           8.3 / 10.2,  1000: 14.4 / 14.1,  2000: 27.1 / 18.2,  4000: 45.6 /  26.8
+    //   1B shape, 8 x 8 nodes (128 tiles)    200           7.2 /  8.7,  1000:  9.8 / 13.1,  2000: 16.2 / 17.9,  4000: 25.1 /  26.8
+    //   8B shape, 4 x 33 nodes (288 tiles)                             1300: 37   / 19
+    //   8B shape, 4 x 64 nodes (512 tiles)    50          25.7 / 20.3
+    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 50.9 / 57.9), and two tiles of more units than the
+    // device has SMs go in one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 88 / 104).
+    const int64_t units = (int64_t)a.kv.nkv * x->batch, tile_pages = units * tiles * pages * a.kv.hd / 128;
+    const int n_sms = current_sms();
+    if (!n_sms) return DEL_ECUDA;
+    const bool waves = units * tiles > (a.kv.hd == 64 ? 2 : 1) * n_sms;      // (of mma.sync CTAs)
+    if (tiles > 1 && (waves || tile_pages > 6000) && !(tiles == 2 && units > n_sms))
+        return launch_tree_attention_tc(a, x->batch, len, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
+    cudaError_t e = a.kv.hd == 128 ? launch<128>(a, x->batch, pages, (cudaStream_t)cuda_stream) : launch<64>(a, x->batch, pages, (cudaStream_t)cuda_stream);
     return e == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }

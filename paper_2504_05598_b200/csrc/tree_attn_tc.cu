@@ -607,27 +607,25 @@ bool make_maps(const PageView &kv, Maps *m) {
 }
 
 template <int HD, int TILES>
-cudaError_t launch(const Maps &m, const TreeArgs &a, int batch, int max_len, int n_sms, cudaStream_t st) {
+cudaError_t launch(const Maps &m, const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
     auto kern = tree_attention_tc_kernel<HD, TILES>;
     static SmemAttrOnce attr;
     cudaError_t e = attr.set(kern, Cfg<HD, TILES>::SMEM);
     if (e != cudaSuccess) return e;
     const int group = a.nh / a.kv.nkv, n_rt = (a.max_nodes * group + TILES * BQ - 1) / (TILES * BQ);
-    // one CTA per SM: as many parts of the keys as one wave holds
-    const int64_t units = (int64_t)a.kv.nkv * n_rt * batch;
+    // as many parts of the keys as are resident together, none for three blocks and less: joining parts costs as much as two blocks
+    static ClusterRoom room;
     const int blocks = (max_len + a.max_nodes + BKEY - 1) / BKEY;
-    int splits = (int)(n_sms / units < 8 ? n_sms / units : 8);
-    if (splits > blocks) splits = blocks;
-    if (splits < 1) splits = 1;
+    const int splits = blocks <= 3 ? 1 : room.best(kern, Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, (int64_t)a.kv.nkv * n_rt * batch, blocks);
     return launch_cluster(kern, dim3(splits, a.kv.nkv * n_rt, batch), Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, splits, st, m, a);
 }
 
 }  // namespace
 
-cudaError_t launch_tree_attention_tc(const TreeArgs &a, int batch, int max_len, int n_sms, cudaStream_t st) {
+cudaError_t launch_tree_attention_tc(const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
     Maps m;
     if (!make_maps(a.kv, &m)) return cudaErrorInvalidValue;
     const bool one = a.max_nodes * (a.nh / a.kv.nkv) <= BQ;
-    if (a.kv.hd == 128) return one ? launch<128, 1>(m, a, batch, max_len, n_sms, st) : launch<128, 2>(m, a, batch, max_len, n_sms, st);
-    return one ? launch<64, 1>(m, a, batch, max_len, n_sms, st) : launch<64, 2>(m, a, batch, max_len, n_sms, st);
+    if (a.kv.hd == 128) return one ? launch<128, 1>(m, a, batch, max_len, st) : launch<128, 2>(m, a, batch, max_len, st);
+    return one ? launch<64, 1>(m, a, batch, max_len, st) : launch<64, 2>(m, a, batch, max_len, st);
 }

@@ -38,7 +38,7 @@ BAD_PAGES = [dict(k_pages=None), dict(v_pages=P + 8), dict(n_pages=0), dict(n_la
 
 @pytest.mark.parametrize("over", [dict(q=None), dict(out=None), dict(page_table=None), dict(lens=None), dict(q=P + 2), dict(out=P + 8), dict(out_lo=P + 8),
                                   dict(lens=P + 2), dict(mask=P + 4), dict(q_node_stride=257), dict(out_seq_stride=4), dict(batch=0), dict(batch=65536),
-                                  dict(max_nodes=0), dict(max_nodes=65), dict(n_heads=3), dict(n_heads=0), dict(layer=0), dict(layer=3),
+                                  dict(max_nodes=0), dict(max_nodes=65), dict(n_heads=3), dict(n_heads=0), dict(n_heads=2050), dict(layer=0), dict(layer=3),
                                   dict(table_cols=0), dict(table_cols=1 << 28), dict(table_stride=-1), dict(max_len=-1), dict(scale=-1.0),
                                   dict(scale=float("nan")), dict(scale=float("inf"))])
 def test_tree_attention_refuses(over):
