@@ -172,6 +172,24 @@ int del_select(del_ctx *ctx, int seq, int32_t *E, int32_t *gamma);
  * DEL_ESTATE if no sequence is live. */
 int del_round(del_ctx *ctx, del_round_out *out);
 
+/* Verifies a tree of drafts that the caller proposes (from another model, a table, several exits): one pass of n_drafts + 1 rows
+ * through all layers.  tokens, parents: HOST int32 [n_drafts]; draft i follows draft parents[i] < i, or the token that the next round would
+ * feed (parents[i] = -1); 0 <= n_drafts < DEL_MAX_ROWS.  A node sees the committed positions and its ancestors, and is rotated by its
+ * depth.  Greedy: starting at the root, the target's top-1 token is emitted, and the walk goes on at the child that carries it (of
+ * several the first).  The keys and values of the path are moved together and committed.  out_tokens (HOST int32 [n_drafts + 1]) gets
+ * the n_emitted tokens: at least 1, at most the depth of the tree + 1 and what is left of max_new_tokens.  Statistics and the choice of the next
+ * (E, gamma), which are about drafts of the exit layers, stay as they are; rounds of both kinds may follow one another.  Synchronises.
+ * Errors: DEL_EINVAL, DEL_ESTATE (no prefill, finished, a round half done, or the slot samples), DEL_ENOSPC, DEL_ETIMEOUT. */
+int del_verify_tree(del_ctx *ctx, int seq, int n_drafts, const int32_t *tokens, const int32_t *parents, int32_t *out_tokens,
+                    int32_t *n_emitted);
+
+/* Continues a sequence in a second slot as well (several answers from one prompt): `to` (released first) gets the committed positions of
+ * `from`, its next token, statistics, policy and exit mode, and max_new_tokens (>= 1) tokens of its own.  Full pages are shared until both
+ * are released; the part-filled last page is copied.  Sampling belongs to the slot: with a seed of its own each continues on its own.  What
+ * the readers of the last round return is not carried over.  Synchronises.  Errors: DEL_EINVAL, DEL_ESTATE (`from` not prefilled or
+ * its round half done), DEL_ENOSPC. */
+int del_fork(del_ctx *ctx, int from, int to, int max_new_tokens);
+
 /* Fix the policy of a sequence: del_round uses (E, gamma) as given instead of the selection
  * (gamma = 0: plain auto-regressive decoding).  E <= 0 restores the dynamic choice. */
 int del_set_policy(del_ctx *ctx, int seq, int E, int gamma);

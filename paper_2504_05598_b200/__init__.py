@@ -31,7 +31,7 @@ EXPORTS = ["del_workspace_bytes", "del_init", "del_prefill", "del_draft", "del_v
            "del_get_drafts", "del_force_token", "del_get_hidden", "del_debug_logits", "del_get_kv", "del_committed_len", "del_release",
            "del_launch_count", "del_get_traffic", "del_set_flags", "del_get_kernel_times", "del_head_argmax_static",
            "del_set_policy_fs", "del_set_exit_mode", "del_get_window", "del_set_sampling", "del_get_sample_info", "del_get_round_logits", "del_sample_probe", "del_get_conf_stats", "del_set_conf_stats", "del_get_conf", "del_debug_inject_error", "del_debug_routes",
-           "del_tree_attention", "del_kv_compact", "del_kv_fork", "del_beam_select", "del_beam_workspace_bytes", "del_strerror", "del_last_cuda_error", "del_destroy"]
+           "del_tree_attention", "del_kv_compact", "del_kv_fork", "del_beam_select", "del_beam_workspace_bytes", "del_verify_tree", "del_fork", "del_strerror", "del_last_cuda_error", "del_destroy"]
 
 
 class Shape(C.Structure):
@@ -117,6 +117,10 @@ def load_library(build_if_missing: bool = True):
     L.del_verify.argtypes = [vp, ci]
     L.del_layer_accept.restype = ci
     L.del_layer_accept.argtypes = [vp, ci, C.POINTER(RoundOut)]
+    L.del_verify_tree.restype = ci
+    L.del_verify_tree.argtypes = [vp, ci, ci, vp, vp, vp, vp]
+    L.del_fork.restype = ci
+    L.del_fork.argtypes = [vp, ci, ci, ci]
     L.del_select.restype = ci
     L.del_select.argtypes = [vp, ci, C.POINTER(i32), C.POINTER(i32)]
     L.del_round.restype = ci
@@ -317,6 +321,19 @@ class DelContext:
     def try_round(self):
         outs = (RoundOut * self.shape.max_batch)()
         return self.lib.del_round(self._h, outs), list(outs)
+
+    def verify_tree(self, seq: int, tokens: Sequence[int], parents: Sequence[int]) -> List[int]:
+        """One round that verifies a proposed tree of drafts (draft i follows draft parents[i], or the last token: -1); the emitted tokens."""
+        t, p = (np.ascontiguousarray(x, dtype=np.int32) for x in (tokens, parents))
+        if t.ndim != 1 or t.shape != p.shape:
+            raise DelError(EINVAL, "del_verify_tree", "tokens and parents: one entry per draft expected")
+        out, n = np.zeros(len(t) + 1, dtype=np.int32), C.c_int32()
+        self._ck(self.lib.del_verify_tree(self._h, seq, len(t), t.ctypes.data, p.ctypes.data, out.ctypes.data, C.addressof(n)), "del_verify_tree")
+        return out[: n.value].tolist()
+
+    def fork(self, from_seq: int, to_seq: int, max_new_tokens: int):
+        """Continues a sequence in a second slot as well, sharing its full pages."""
+        self._ck(self.lib.del_fork(self._h, from_seq, to_seq, max_new_tokens), "del_fork")
 
     def set_policy(self, seq: int, E: int, gamma: int):
         self._ck(self.lib.del_set_policy(self._h, seq, E, gamma), "del_set_policy")

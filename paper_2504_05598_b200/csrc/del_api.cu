@@ -3,9 +3,12 @@
 // here: every buffer is carved out of the caller's workspace.
 #include "../../include/del.h"
 #include "kernels.h"
+#include "pages.cuh"
+#include "tree_attn.cuh"
 
 #include <algorithm>
 #include <chrono>
+#include <cstddef>
 #include <cstdio>
 #include <cstring>
 #include <new>
@@ -34,6 +37,13 @@ struct SeqHost {
     double tau = 0.0;        // Eq. 3 threshold of the exit layer the next round uses
     double cur_tau = 0.0;
     std::vector<int> pages;
+};
+
+// device copy of what a tree or a fork needs, uploaded in one piece each
+struct TreeDev {
+    uint64_t mask[DEL_ROWS_MAX];
+    int32_t len, nodes, pad[2];
+    int32_t src_pos[DEL_ROWS_MAX], count, dst_start, pad2[2];
 };
 
 struct Carve {
@@ -70,6 +80,8 @@ struct del_ctx {
     del_round_out *out_host = nullptr, *out_dev = nullptr; // [B]
     void *stage_host = nullptr;                            // small pinned scratch
     float *dbg_dev = nullptr;                              // [V] debug logits / kv rows
+    TreeDev *tree_dev = nullptr;                           // inputs of the tree attention and the compaction of del_verify_tree / del_fork
+    std::vector<int> page_refs;                            // sequences that hold a page
     alignas(64) unsigned char map_x[128], map_w[128];     // tensor maps of the stacked rows and of W_lm
     // bulk prefill on the tensor cores: chunk buffers in the workspace, tensor maps of them and of every layer's weights
     struct TMap { alignas(64) unsigned char b[128]; };
@@ -116,7 +128,7 @@ namespace {
 int prefill_rows(const del_shape &s) { return std::min(PF_ROWS, (s.max_seq + 127) / 128 * 128); }
 
 size_t carve_all(const del_shape &s, int pf_rows, void *base, Dims &D, Buffers &B, int &R_max, int &n_vtiles,
-                 del_round_out **out_dev, float **dbg_dev, PfArgs *pf, WtBuffers *wt) {
+                 del_round_out **out_dev, float **dbg_dev, TreeDev **tree_dev, PfArgs *pf, WtBuffers *wt) {
     D.L = s.n_layers; D.d = s.d_model; D.nh = s.n_heads; D.nkv = s.n_kv_heads; D.hd = s.head_dim; D.F = s.d_ffn; D.V = s.vocab;
     D.B = s.max_batch;
     // slots of the hidden stack per sequence: what a round needs (g_max + 1 rows, the prefill window), raised to
@@ -176,6 +188,7 @@ size_t carve_all(const del_shape &s, int pf_rows, void *base, Dims &D, Buffers &
     *out_dev = c.take<del_round_out>(base, (size_t)D.B);
     B.ERR = c.take<int32_t>(base, 64);           // right behind the results: one copy brings both to the host
     *dbg_dev = c.take<float>(base, (size_t)std::max(D.V, 2 * D.nkv * D.hd));
+    *tree_dev = c.take<TreeDev>(base, 1);
     // chunk buffers of the bulk prefill (pf_rows prompt positions)
     PfArgs pfa;
     memset(&pfa, 0, sizeof(pfa));
@@ -205,8 +218,8 @@ size_t carve_all(const del_shape &s, int pf_rows, void *base, Dims &D, Buffers &
 }
 
 size_t workspace_bytes(const del_shape &s, int pf_rows) {
-    Dims D; Buffers B; int R, nv; del_round_out *o; float *dbg;
-    return carve_all(s, pf_rows, nullptr, D, B, R, nv, &o, &dbg, nullptr, nullptr);
+    Dims D; Buffers B; int R, nv; del_round_out *o; float *dbg; TreeDev *t;
+    return carve_all(s, pf_rows, nullptr, D, B, R, nv, &o, &dbg, &t, nullptr, nullptr);
 }
 
 // the most chunk rows that fit into ws_bytes; 0: not even one tile of them
@@ -325,7 +338,7 @@ void fill_plan(const del_ctx *c, PassPlan *p, const std::vector<RowSpec> &specs,
         p->seg[ns++] = Segment{r.seq, m, r.nrows, s.T + r.slot0};
         for (int i = 0; i < r.nrows; ++i) {
             const int slot = r.slot0 + i, pos = s.T + slot;
-            p->rows[m++] = RowDesc{r.seq, slot, pos, prompt_tokens ? pos : r.seq * (c->D.S + 1) + slot};
+            p->rows[m++] = RowDesc{r.seq, slot, pos, prompt_tokens ? pos : r.seq * (c->D.S + 1) + slot, pos};
         }
     }
     p->m = m;
@@ -342,6 +355,7 @@ int ensure_pages(del_ctx *c, int sq, int positions) {
     while ((int)s.pages.size() < need) {
         const int pg = c->free_pages.back();
         c->free_pages.pop_back();
+        c->page_refs[pg] = 1;
         c->pt_host[(size_t)sq * c->D.pages_per_seq + s.pages.size()] = pg;
         s.pages.push_back(pg);
     }
@@ -355,7 +369,8 @@ int ensure_pages(del_ctx *c, int sq, int positions) {
 
 void release_seq(del_ctx *c, int sq) {
     SeqHost &s = c->seq[sq];
-    for (int pg : s.pages) c->free_pages.push_back(pg);
+    for (int pg : s.pages)
+        if (--c->page_refs[pg] == 0) c->free_pages.push_back(pg);
     s = SeqHost();
 }
 
@@ -433,8 +448,8 @@ PassInfo pass_info(const del_ctx *c, int plan_idx) {
     return pi;
 }
 
-// one decoder layer over the rows of a pass
-int run_layer(del_ctx *c, const PassInfo &pi, int l, bool write_exit, bool first) {
+// one decoder layer over the rows of a pass (tree: they are the nodes of a tree, whose attention this is)
+int run_layer(del_ctx *c, const PassInfo &pi, int l, bool write_exit, bool first, const TreeArgs *tree = nullptr) {
     const Dims &D = c->D;
     const bool P = pdl(c);
     // the layer before left its output by row of this pass as well
@@ -457,7 +472,12 @@ int run_layer(del_ctx *c, const PassInfo &pi, int l, bool write_exit, bool first
             LAUNCH(launch_rowgemm(EPI_QKV, a, pi.m, c->n_sms, c->st, P));
         }
     }
-    {
+    if (tree) {
+        TreeArgs a = *tree;
+        a.layer = l;
+        TAG(CLS_ATTN, 4.0 * pi.max_kv * D.nkv * D.hd);
+        LAUNCH(launch_tree_attention(a, 1, pi.max_kv, c->st));
+    } else {
         AttnArgs a;
         memset(&a, 0, sizeof(a));
         a.D = D; a.B = c->B; a.plan = c->plan_host[pi.plan_idx]; a.layer = l;
@@ -1067,8 +1087,8 @@ size_t del_workspace_bytes(const del_shape *shape) {
 
 int del_debug_routes(const del_shape *shape, int n_sms, int n_prompt, int rows, int32_t *out) {
     if (validate(shape) != DEL_OK || n_sms < 1 || n_prompt < 1 || rows < 1 || !out) return DEL_EINVAL;
-    Dims D; Buffers B; int R, nv; del_round_out *o; float *dbg;
-    carve_all(*shape, prefill_rows(*shape), nullptr, D, B, R, nv, &o, &dbg, nullptr, nullptr);
+    Dims D; Buffers B; int R, nv; del_round_out *o; float *dbg; TreeDev *t;
+    carve_all(*shape, prefill_rows(*shape), nullptr, D, B, R, nv, &o, &dbg, &t, nullptr, nullptr);
     out[0] = rowgemm_tc_supported(D) ? rows_min_tc(D) : DEL_ROWS_MAX + 1;
     out[1] = prefill_tc_chunk(D, n_prompt, n_sms, prefill_rows(*shape));
     for (int epi = PF_QKV; epi <= PF_DOWN; ++epi) {
@@ -1095,7 +1115,7 @@ int del_init(del_ctx **out, const del_shape *shape, const del_weights *w, const 
     if (!c) return DEL_ENOSPC;
     c->sh = *shape;
     c->pf_rows = pf_rows;
-    carve_all(*shape, pf_rows, workspace, c->D, c->B, c->R_max, c->n_vtiles, &c->out_dev, &c->dbg_dev, &c->pf, &c->wt);
+    carve_all(*shape, pf_rows, workspace, c->D, c->B, c->R_max, c->n_vtiles, &c->out_dev, &c->dbg_dev, &c->tree_dev, &c->pf, &c->wt);
     c->B.KP = (bf16 *)kv->k_pages; c->B.VP = (bf16 *)kv->v_pages; c->B.PT = kv->page_table;
     c->B.rope_cos = w->rope_cos; c->B.rope_sin = w->rope_sin;
     c->tok_emb = (const bf16 *)w->tok_emb; c->final_norm = (const bf16 *)w->final_norm; c->lm_head = (const bf16 *)w->lm_head;
@@ -1209,6 +1229,7 @@ int del_init(del_ctx **out, const del_shape *shape, const del_weights *w, const 
     }
     c->pt_host.assign((size_t)c->D.B * c->D.pages_per_seq, 0);
     for (int p = shape->n_pages - 1; p >= 0; --p) c->free_pages.push_back(p);
+    c->page_refs.assign(shape->n_pages, 0);
     *out = c;
     return DEL_OK;
 }
@@ -1437,6 +1458,219 @@ int del_round(del_ctx *c, del_round_out *out) {
         if (rc) return rc;
     }
     for (const Job &j : jobs) finish_round(c, j.seq, &out[j.seq], true);
+    return DEL_OK;
+}
+
+// arg-max tokens of the last layer's rows 0..n-1 of a sequence -> B.SHADOW
+static int last_layer_tokens(del_ctx *c, int sq, int n) {
+    UpdatePlan *up = &c->up_host[0];
+    memset(up, 0, sizeof(*up));
+    up->lay_first = 1;
+    up->lay_n = 1;                            // the last layer alone
+    up->n_seq = 1;
+    up->s[0].seq = sq;
+    up->s[0].g = n - 1;
+    up->s[0].E = 1;
+    up->n_rows = n;
+    const bool P = pdl(c);
+    CtlArgs ca = ctl_base(c, -1);
+    ca.n_rows = n;
+    LAUNCH(launch_prep_rows(ca, up, n, c->st, P));
+    if ((c->flags & FLAG_TC) && c->tc_ok) {
+        const int nvt = lmhead_tc_vtiles(c->D.V);
+        TAG(CLS_LMSTACK, 2.0 * c->D.V * c->D.d);
+        LAUNCH(launch_lmhead_tc(c->map_x, c->map_w, c->B.TPV, c->B.TPI, c->B.TPS, c->B.RS, n, c->D.V, c->D.d, c->B.ERR, nullptr, 0, c->n_sms, c->st, P));
+        LAUNCH(launch_shadow_reduce(ca, up, c->B.TPV, c->B.TPI, c->B.TPS, nvt, 1, nvt, 0, n, c->st, P));
+        return DEL_OK;
+    }
+    int rc = plan_begin(c, 1);
+    if (rc) return rc;
+    PlanBatch pb(c);
+    int idx;
+    PassPlan *p = pb.add(&idx);
+    memset(p, 0, sizeof(*p));
+    p->m = n;
+    rc = plan_commit(c, pb);
+    if (rc) return rc;
+    GemmArgs a = gemm_base(c, idx, 0);
+    a.K = c->D.d;
+    a.n_items = c->D.V / 16;
+    a.X = c->B.XN;
+    a.W0 = c->lm_head;
+    a.x_by_row = 1;
+    a.row_scale = c->B.RS;
+    TAG(CLS_LMSTACK, 2.0 * c->D.V * c->D.d);
+    LAUNCH(launch_rowgemm(EPI_LMHEAD, a, n, c->n_sms, c->st, P));
+    LAUNCH(launch_shadow_reduce(ca, up, c->B.LPV, c->B.LPI, c->B.LPS, rowgemm_lmhead_grid(a.n_items, n, c->n_sms, a.ctas_per_sm), DEL_ROWS_MAX, 1, 0, n, c->st, P));
+    return DEL_OK;
+}
+
+// positions src_pos[0 .. n) of a sequence's table to positions start.. of another's (tree_dev->src_pos, count, dst_start are uploaded here)
+static int move_positions(del_ctx *c, int from, int to, const int32_t *src_pos, int n, int start) {
+    TreeDev *t = reinterpret_cast<TreeDev *>(reinterpret_cast<char *>(c->stage_host) + 32768);
+    memcpy(t->src_pos, src_pos, sizeof(int32_t) * n);
+    t->count = n;
+    t->dst_start = start;
+    const size_t off = offsetof(TreeDev, src_pos);
+    CK(cudaMemcpyAsync(c->tree_dev->src_pos, t->src_pos, sizeof(TreeDev) - off, cudaMemcpyHostToDevice, c->st));
+    c->h2d_bytes += sizeof(TreeDev) - off;
+    const Dims &D = c->D;
+    del_compact x;
+    memset(&x, 0, sizeof(x));
+    x.src_table = c->B.PT + (size_t)from * D.pages_per_seq;
+    x.dst_table = c->B.PT + (size_t)to * D.pages_per_seq;
+    x.src_pos = c->tree_dev->src_pos;
+    x.counts = &c->tree_dev->count;
+    x.dst_start = &c->tree_dev->dst_start;
+    x.batch = 1;
+    x.max_count = n;
+    x.src_cols = x.dst_cols = x.src_stride = x.dst_stride = D.pages_per_seq;
+    x.pos_stride = DEL_ROWS_MAX;
+    LAUNCH(launch_kv_compact(PageView{c->B.KP, c->B.VP, c->sh.n_pages, D.L, D.nkv, D.hd}, x, c->st));
+    return DEL_OK;
+}
+
+int del_verify_tree(del_ctx *c, int sq, int n_drafts, const int32_t *tokens, const int32_t *parents, int32_t *out_tokens, int32_t *n_emitted) {
+    if (!seq_ok(c, sq) || n_drafts < 0 || n_drafts >= DEL_ROWS_MAX || (n_drafts && (!tokens || !parents)) || !out_tokens || !n_emitted) return DEL_EINVAL;
+    for (int i = 0; i < n_drafts; ++i)
+        if (tokens[i] < 0 || tokens[i] >= c->D.V || parents[i] < -1 || parents[i] >= i) return DEL_EINVAL;
+    SeqHost &s = c->seq[sq];
+    *n_emitted = 0;
+    if (!s.active || s.remaining < 1 || s.phase != 0 || samples(c, sq)) return DEL_ESTATE;
+    const Dims &D = c->D;
+    const int n = n_drafts + 1;                                   // node 0: the token that the next round feeds
+    int rc = ensure_pages(c, sq, s.T + n);
+    if (rc) return rc;
+    // what each node sees, its depth
+    TreeDev *t = reinterpret_cast<TreeDev *>(reinterpret_cast<char *>(c->stage_host) + 40960);
+    int depth[DEL_ROWS_MAX];
+    t->mask[0] = 1;
+    depth[0] = 0;
+    for (int i = 1; i < n; ++i) {
+        t->mask[i] = t->mask[parents[i - 1] + 1] | (1ull << i);
+        depth[i] = depth[parents[i - 1] + 1] + 1;
+    }
+    t->len = s.T;
+    t->nodes = n;
+    CK(cudaMemcpyAsync(c->tree_dev, t, offsetof(TreeDev, src_pos), cudaMemcpyHostToDevice, c->st));
+    c->h2d_bytes += offsetof(TreeDev, src_pos);
+    if (n_drafts) {
+        int32_t *tok = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(c->stage_host) + 49152);
+        memcpy(tok, tokens, sizeof(int32_t) * n_drafts);
+        CK(cudaMemcpyAsync(c->B.TOK + (size_t)sq * (D.S + 1) + 1, tok, sizeof(int32_t) * n_drafts, cudaMemcpyHostToDevice, c->st));
+        c->h2d_bytes += sizeof(int32_t) * n_drafts;
+    }
+    c->in_round = true;
+    rc = plan_begin(c, 1);
+    if (rc) return rc;
+    PlanBatch pb(c);
+    int idx;
+    PassPlan *p = pb.add(&idx);
+    fill_plan(c, p, {RowSpec{sq, 0, n}}, false);
+    for (int i = 0; i < n; ++i) p->rows[i].rpos = s.T + depth[i];
+    rc = plan_commit(c, pb);
+    if (rc) return rc;
+    LAUNCH(launch_embed(ctl_base(c, idx), n, c->st, pdl(c)));
+    TreeArgs ta;
+    memset(&ta, 0, sizeof(ta));
+    ta.kv = PageView{c->B.KP, c->B.VP, c->sh.n_pages, D.L, D.nkv, D.hd};
+    ta.q = c->B.Q; ta.out = c->B.ATT; ta.out_lo = c->B.ATTL;
+    ta.table = c->B.PT + (size_t)sq * D.pages_per_seq;
+    ta.lens = &c->tree_dev->len; ta.nodes = &c->tree_dev->nodes; ta.mask = c->tree_dev->mask;
+    ta.err = c->B.ERR;
+    ta.q_node = ta.o_node = (int64_t)D.nh * D.hd;
+    ta.max_nodes = n; ta.nh = D.nh; ta.cols = ta.stride = D.pages_per_seq;
+    ta.scale = rsqrtf((float)D.hd) * 1.4426950408889634f;
+    const PassInfo pi = pass_info(c, idx);
+    for (int l = 1; l <= D.L; ++l) {
+        rc = run_layer(c, pi, l, false, l == 1, &ta);
+        if (rc) return rc;
+    }
+    rc = last_layer_tokens(c, sq, n);
+    if (rc) return rc;
+    // the target's token at every node, and the error word
+    int32_t *got = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(c->stage_host) + 57344);
+    CK(cudaMemcpyAsync(got, c->B.SHADOW + ((size_t)sq * D.L + (D.L - 1)) * D.S, sizeof(int32_t) * n, cudaMemcpyDeviceToHost, c->st));
+    c->d2h_bytes += sizeof(int32_t) * n;
+    rc = read_out(c);
+    if (rc) return rc;
+    // the path that the target's own tokens take through the tree
+    int32_t path[DEL_ROWS_MAX], emitted[DEL_ROWS_MAX];
+    int k = 0;
+    for (int cur = 0;;) {
+        path[k] = s.T + cur;
+        emitted[k] = got[cur];
+        ++k;
+        int next = -1;
+        for (int i = n - 1; i > cur; --i)
+            if (parents[i - 1] + 1 == cur && tokens[i - 1] == got[cur]) next = i;
+        if (next < 0 || k == s.remaining) break;
+        cur = next;
+    }
+    // its keys and values move together; the root stays, and so does what has only nodes of the path before it
+    int first = 1;
+    while (first < k && path[first] == s.T + first) ++first;
+    if (first < k) {
+        rc = move_positions(c, sq, sq, path + first, k - first, s.T + first);
+        if (rc) return rc;
+    }
+    int32_t *last = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(c->stage_host) + 61440);
+    *last = emitted[k - 1];
+    CK(cudaMemcpyAsync(c->B.TOK + (size_t)sq * (D.S + 1), last, sizeof(int32_t), cudaMemcpyHostToDevice, c->st));
+    c->h2d_bytes += sizeof(int32_t);
+    CK(cudaStreamSynchronize(c->st));        // (the next round's attention reads committed positions before it waits for its producer)
+    memcpy(out_tokens, emitted, sizeof(int32_t) * k);
+    *n_emitted = k;
+    s.T += k;
+    s.remaining -= k;
+    return DEL_OK;
+}
+
+int del_fork(del_ctx *c, int from, int to, int max_new_tokens) {
+    if (!seq_ok(c, from) || !seq_ok(c, to) || from == to || max_new_tokens < 1) return DEL_EINVAL;
+    const SeqHost &src = c->seq[from];
+    if (!src.active || src.phase != 0) return DEL_ESTATE;
+    const Dims &D = c->D;
+    if (src.T + max_new_tokens + c->sh.g_max + 1 > D.max_seq) return DEL_ENOSPC;
+    const int full = src.T / 16, part = src.T % 16;
+    {
+        // a page of its own for the part-filled last one, from the free ones or from what `to` holds alone
+        size_t room = c->free_pages.size();
+        for (int pg : c->seq[to].pages) room += c->page_refs[pg] == 1;
+        if (part && room == 0) return DEL_ENOSPC;
+    }
+    release_seq(c, to);
+    SeqHost &dst = c->seq[to];
+    dst = src;
+    dst.pages.assign(src.pages.begin(), src.pages.begin() + full);
+    dst.remaining = max_new_tokens;
+    dst.active = false;                       // until everything is there
+    for (int p = 0; p < full; ++p) {
+        ++c->page_refs[dst.pages[p]];
+        c->pt_host[(size_t)to * D.pages_per_seq + p] = dst.pages[p];
+    }
+    if (full) {
+        CK(cudaMemcpyAsync(c->B.PT + (size_t)to * D.pages_per_seq, c->pt_host.data() + (size_t)to * D.pages_per_seq, sizeof(int32_t) * full, cudaMemcpyHostToDevice, c->st));
+        c->h2d_bytes += sizeof(int32_t) * full;
+    }
+    if (part) {
+        int rc = ensure_pages(c, to, src.T);
+        if (rc) { release_seq(c, to); return rc; }
+        int32_t pos[16];
+        for (int i = 0; i < part; ++i) pos[i] = full * 16 + i;
+        rc = move_positions(c, from, to, pos, part, full * 16);
+        if (rc) { release_seq(c, to); return rc; }
+    }
+    // the token to feed next, statistics and the choice for the next round
+    auto copy = [&](auto *base, size_t row) { return cudaMemcpyAsync(base + to * row, base + from * row, sizeof(*base) * row, cudaMemcpyDeviceToDevice, c->st); };
+    CK(cudaMemcpyAsync(c->B.TOK + (size_t)to * (D.S + 1), c->B.TOK + (size_t)from * (D.S + 1), sizeof(int32_t), cudaMemcpyDeviceToDevice, c->st));
+    CK(copy(c->B.ST, 1));
+    CK(copy(c->B.SC, D.L));
+    CK(copy(c->B.STCS, D.L));
+    CK(copy(c->B.SFCS, D.L));
+    CK(copy(c->B.TAU, D.L));
+    CK(cudaStreamSynchronize(c->st));        // (as in del_verify_tree)
+    dst.active = true;
     return DEL_OK;
 }
 

@@ -330,32 +330,35 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
 
 }  // namespace
 
-extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *cuda_stream) {
-    CompactArgs a;
-    if (!x || !page_view(kv, &a.kv)) return DEL_EINVAL;
-    if (!x->src_table || !x->dst_table || !x->src_pos || !x->counts || !x->dst_start) return DEL_EINVAL;
-    if (((uintptr_t)x->src_table | (uintptr_t)x->dst_table | (uintptr_t)x->src_pos | (uintptr_t)x->counts | (uintptr_t)x->dst_start) & 3) return DEL_EINVAL;
-    if (x->batch < 1 || x->batch > 65535 || x->max_count < 1 || x->src_cols < 1 || x->dst_cols < 1) return DEL_EINVAL;
-    if (x->src_stride < 0 || x->dst_stride < 0 || x->pos_stride < 0) return DEL_EINVAL;
-    a.c = *x;
-    cudaStream_t st = (cudaStream_t)cuda_stream;
+cudaError_t launch_kv_compact(const PageView &kv, const del_compact &x, cudaStream_t st) {
+    CompactArgs a{kv, x, 0};
     // a warp for each destination page of a round; positions of up to max_count / 16 + 2 pages
-    const int n_sms = current_sms(), pages = (x->max_count + 14) / 16 + 1, warps = pages < CP_WARPS ? pages : CP_WARPS;
-    if (!n_sms) return DEL_ECUDA;
-    const int64_t units = (int64_t)a.kv.L * a.kv.nkv * x->batch, rounds = (pages + warps - 1) / warps;
+    const int n_sms = current_sms(), pages = (x.max_count + 14) / 16 + 1, warps = pages < CP_WARPS ? pages : CP_WARPS;
+    if (!n_sms) return cudaErrorInvalidDevice;
+    const int64_t units = (int64_t)a.kv.L * a.kv.nkv * x.batch, rounds = (pages + warps - 1) / warps;
     int64_t parts = 1;
-    if (x->src_table != x->dst_table) {
+    if (x.src_table != x.dst_table) {
         parts = (6 * n_sms + units - 1) / units;
         parts = parts < rounds ? parts : rounds;
     }
     a.stages = (pages + parts - 1) / parts <= warps ? 1 : 2;
-    const dim3 grid(a.kv.L * a.kv.nkv, x->batch, (unsigned)parts);
+    const dim3 grid(a.kv.L * a.kv.nkv, x.batch, (unsigned)parts);
     static SmemAttrOnce attr128, attr64;
-    if ((a.kv.hd == 128 ? attr128.set(compact_kernel<128>, 2 * CP_WARPS * Compact<128>::STAGE) : attr64.set(compact_kernel<64>, 2 * CP_WARPS * Compact<64>::STAGE)) != cudaSuccess)
-        return DEL_ECUDA;
+    const cudaError_t e = a.kv.hd == 128 ? attr128.set(compact_kernel<128>, 2 * CP_WARPS * Compact<128>::STAGE) : attr64.set(compact_kernel<64>, 2 * CP_WARPS * Compact<64>::STAGE);
+    if (e != cudaSuccess) return e;
     if (a.kv.hd == 128) compact_kernel<128><<<grid, warps * 32, a.stages * warps * Compact<128>::STAGE, st>>>(a);
     else compact_kernel<64><<<grid, warps * 32, a.stages * warps * Compact<64>::STAGE, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? DEL_OK : DEL_ECUDA;
+    return cudaGetLastError();
+}
+
+extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *cuda_stream) {
+    PageView view;
+    if (!x || !page_view(kv, &view)) return DEL_EINVAL;
+    if (!x->src_table || !x->dst_table || !x->src_pos || !x->counts || !x->dst_start) return DEL_EINVAL;
+    if (((uintptr_t)x->src_table | (uintptr_t)x->dst_table | (uintptr_t)x->src_pos | (uintptr_t)x->counts | (uintptr_t)x->dst_start) & 3) return DEL_EINVAL;
+    if (x->batch < 1 || x->batch > 65535 || x->max_count < 1 || x->src_cols < 1 || x->dst_cols < 1) return DEL_EINVAL;
+    if (x->src_stride < 0 || x->dst_stride < 0 || x->pos_stride < 0) return DEL_EINVAL;
+    return launch_kv_compact(view, *x, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }
 
 extern "C" int del_kv_fork(const del_pages *kv, const del_fork_args *x, void *cuda_stream) {

@@ -23,6 +23,9 @@ inline bool page_view(const del_pages *kv, PageView *v) {
     return true;
 }
 
+// del_kv_compact behind its checks (kv_pages.cu)
+cudaError_t launch_kv_compact(const PageView &kv, const del_compact &x, cudaStream_t st);
+
 // SMs of the current device (0: the query failed)
 inline int current_sms() {
     static int n[DEL_MAX_DEVICES] = {};

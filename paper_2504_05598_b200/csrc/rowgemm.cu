@@ -234,8 +234,8 @@ __global__ void __launch_bounds__(NW * 32, (NW == 8 && NT <= 4 ? 2 : 1)) rowgemm
             if (cl < NR && c < m && i < 8 && item < nq + nk) {
                 const int it = item < nq ? item : item - nq;
                 const int j = (it - (it / h8) * h8) * 8 + i;
-                cs_pre = a.B.rope_cos[(size_t)plan->rows[c].pos * half + j];
-                sn_pre = a.B.rope_sin[(size_t)plan->rows[c].pos * half + j];
+                cs_pre = a.B.rope_cos[(size_t)plan->rows[c].rpos * half + j];
+                sn_pre = a.B.rope_sin[(size_t)plan->rows[c].rpos * half + j];
             }
         }
     };
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(NW * 32, (NW == 8 && NT <= 4 ? 2 : 1)) rowgemm
         for (int cl = tid >> 4; cl < NR; cl += NTHREADS / 16) {
             const int c = row0 + cl;                // row of the pass; cl: its column in this launch
             const bool valid = c < m;
-            const RowDesc rd = valid ? plan->rows[c] : RowDesc{0, 0, 0, 0};
+            const RowDesc rd = valid ? plan->rows[c] : RowDesc{0, 0, 0, 0, 0};
             // product with the high parts + product with the low parts
             const float ra = HL ? res[cl * 16 + i] + res[(cl + NR) * 16 + i] : res[cl * 16 + i];
             // rows 8..15 of the tile at the same column (rotary partner / up row), read by threads i < 8 only
@@ -284,8 +284,8 @@ __global__ void __launch_bounds__(NW * 32, (NW == 8 && NT <= 4 ? 2 : 1)) rowgemm
                     const bool isq = item < nq;
                     const int it = isq ? item : item - nq;
                     const int head = it / h8, j = (it - head * h8) * 8 + i;
-                    const float cs = ROPE_PRE ? cs_pre : a.B.rope_cos[(size_t)rd.pos * half + j];
-                    const float sn = ROPE_PRE ? sn_pre : a.B.rope_sin[(size_t)rd.pos * half + j];
+                    const float cs = ROPE_PRE ? cs_pre : a.B.rope_cos[(size_t)rd.rpos * half + j];
+                    const float sn = ROPE_PRE ? sn_pre : a.B.rope_sin[(size_t)rd.rpos * half + j];
                     const float oa = va * cs - vb * sn, ob = vb * cs + va * sn;
                     if (isq) {
                         bf16 *q = a.B.Q + (size_t)c * (a.D.nh * hd) + head * hd + j;

@@ -110,7 +110,7 @@ template <int NP> struct ColInfo {
     int src[NP], dst[NP];        // rows of the hidden stack: residual of the O-projection, output of DOWN
     int er[NP];                  // row of the exit buffers
     int kv[NP];                  // QKV: (page * L + layer - 1) * nkv
-    int pos[NP];
+    int pos[NP], rpos[NP];       // position in the cache, and the one that the rotation is for
     float rs[NP];                // 1/rms
 };
 
@@ -134,7 +134,7 @@ __device__ __forceinline__ void epi_loads(const WtArgs &w, const ColInfo<NP> &ci
         const int hh = D.hd >> 1, j = rr & (hh - 1);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const size_t at = (size_t)ci.pos[col + e] * hh + j;
+            const size_t at = (size_t)ci.rpos[col + e] * hh + j;
             p[e] = e < n && rot ? __ldg(a.B.rope_cos + at) : 0.f;
             p2[e] = e < n && rot ? __ldg(a.B.rope_sin + at) : 0.f;
         }
@@ -381,6 +381,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) rowgemm_tc_kernel(const __grid_
                 ci.dst[col] = src + D.B * D.S;
                 ci.er[col] = rd.seq * D.S + rd.slot;
                 ci.pos[col] = rd.pos;
+                ci.rpos[col] = rd.rpos;
                 if (EPI == EPI_QKV) ci.kv[col] = (a.B.PT[rd.seq * D.pages_per_seq + (rd.pos >> 4)] * D.L + (a.layer - 1)) * D.nkv;
                 ci.rs[col] = rsqrtf(s / (float)D.d + D.eps);
             }

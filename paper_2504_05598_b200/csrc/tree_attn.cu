@@ -244,6 +244,28 @@ cudaError_t launch(const TreeArgs &a, int batch, int pages, cudaStream_t st) {
 
 }  // namespace
 
+cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
+    const int pages = (max_len + a.max_nodes + 15) / 16;
+    // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 256 rows, but starts 2 to 3 us later.
+    // The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync / tcgen05, two kv layers in turn:
+    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions 7.8 /  9.4,  1000:  8.7 / 10.4,  4000: 14.6 / 14.4
+    //   8B shape, 4 x 8 nodes (64 tiles)     200           8.0 /  9.7,  1000: 11.2 / 12.3,  2000: 17.9 / 15.1,  4000: 27.8 /  22.1
+    //   13B shape, 1 x 26 nodes (80 tiles)   200           8.3 / 10.2,  1000: 14.4 / 14.1,  2000: 27.1 / 18.2,  4000: 45.6 /  26.8
+    //   1B shape, 8 x 8 nodes (128 tiles)    200           7.2 /  8.7,  1000:  9.8 / 13.1,  2000: 16.2 / 17.9,  4000: 25.1 /  26.8
+    //   8B shape, 4 x 33 nodes (288 tiles)                             1300: 37   / 19
+    //   8B shape, 4 x 64 nodes (512 tiles)    50          25.7 / 20.3
+    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 50.9 / 57.9), and two tiles of more units than the
+    // device has SMs go in one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 88 / 104).
+    const int64_t tiles = ((int64_t)a.max_nodes * (a.nh / a.kv.nkv) + 15) / 16;
+    const int64_t units = (int64_t)a.kv.nkv * batch, tile_pages = units * tiles * pages * a.kv.hd / 128;
+    const int n_sms = current_sms();
+    if (!n_sms) return cudaErrorInvalidDevice;
+    const bool waves = units * tiles > (a.kv.hd == 64 ? 2 : 1) * n_sms;      // (of mma.sync CTAs)
+    if (tiles > 1 && (waves || tile_pages > 6000) && !(tiles == 2 && units > n_sms))
+        return launch_tree_attention_tc(a, batch, max_len, st);
+    return a.kv.hd == 128 ? launch<128>(a, batch, pages, st) : launch<64>(a, batch, pages, st);
+}
+
 extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, void *cuda_stream) {
     TreeArgs a;
     memset(&a, 0, sizeof(a));
@@ -265,23 +287,5 @@ extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, v
     a.scale = (x->scale > 0.f ? x->scale : 1.f / sqrtf((float)a.kv.hd)) * LOG2E;
     a.err = x->error;
     const int len = x->max_len ? (x->max_len < x->table_cols * 16 ? x->max_len : x->table_cols * 16) : x->table_cols * 16;
-    const int pages = (len + x->max_nodes + 15) / 16;
-    // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 256 rows, but starts 2 to 3 us later.
-    // The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync / tcgen05, two kv layers in turn:
-    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions 7.8 /  9.4,  1000:  8.7 / 10.4,  4000: 14.6 / 14.4
-    //   8B shape, 4 x 8 nodes (64 tiles)     200           8.0 /  9.7,  1000: 11.2 / 12.3,  2000: 17.9 / 15.1,  4000: 27.8 /  22.1
-    //   13B shape, 1 x 26 nodes (80 tiles)   200           8.3 / 10.2,  1000: 14.4 / 14.1,  2000: 27.1 / 18.2,  4000: 45.6 /  26.8
-    //   1B shape, 8 x 8 nodes (128 tiles)    200           7.2 /  8.7,  1000:  9.8 / 13.1,  2000: 16.2 / 17.9,  4000: 25.1 /  26.8
-    //   8B shape, 4 x 33 nodes (288 tiles)                             1300: 37   / 19
-    //   8B shape, 4 x 64 nodes (512 tiles)    50          25.7 / 20.3
-    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 50.9 / 57.9), and two tiles of more units than the
-    // device has SMs go in one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 88 / 104).
-    const int64_t units = (int64_t)a.kv.nkv * x->batch, tile_pages = units * tiles * pages * a.kv.hd / 128;
-    const int n_sms = current_sms();
-    if (!n_sms) return DEL_ECUDA;
-    const bool waves = units * tiles > (a.kv.hd == 64 ? 2 : 1) * n_sms;      // (of mma.sync CTAs)
-    if (tiles > 1 && (waves || tile_pages > 6000) && !(tiles == 2 && units > n_sms))
-        return launch_tree_attention_tc(a, x->batch, len, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
-    cudaError_t e = a.kv.hd == 128 ? launch<128>(a, x->batch, pages, (cudaStream_t)cuda_stream) : launch<64>(a, x->batch, pages, (cudaStream_t)cuda_stream);
-    return e == cudaSuccess ? DEL_OK : DEL_ECUDA;
+    return launch_tree_attention(a, x->batch, len, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }

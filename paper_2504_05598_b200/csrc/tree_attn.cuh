@@ -45,5 +45,7 @@ __device__ __forceinline__ bool sees(uint64_t bits, int tok, int len, int n_keys
 
 }  // namespace tree
 
-// Tiles of up to 256 query rows on tcgen05 (tree_attn_tc.cu).  max_len: what lens are expected to reach.
+// del_tree_attention behind its checks.  max_len: what lens are expected to reach.
+cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st);
+// Tiles of up to 256 query rows on tcgen05 (tree_attn_tc.cu)
 cudaError_t launch_tree_attention_tc(const TreeArgs &a, int batch, int max_len, cudaStream_t st);

@@ -99,3 +99,9 @@ def test_binding_refuses_host_tensors_and_wrong_types():
         dl.kv_fork(k.float(), v, i, i[0, :1], i[0, :1], i[0], i[0], i, i[0, :1], i[0, :2])
     with pytest.raises(dl.DelError):
         dl.beam_select(torch.zeros(1, 1, 8), torch.zeros(1, 1), torch.zeros(1, 2), i[:, :2], i[:, :2])
+
+
+def test_context_calls_without_a_context():
+    lib = dl.load_library()
+    assert lib.del_verify_tree(None, 0, 0, None, None, None, None) == dl.EINVAL
+    assert lib.del_fork(None, 0, 1, 1) == dl.EINVAL
