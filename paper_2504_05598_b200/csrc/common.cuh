@@ -16,10 +16,9 @@
 typedef __nv_bfloat16 bf16;
 
 // One row of a layer pass: which sequence, which slot of the hidden stack, which position of the
-// sequence's cache, where its input token sits in the token buffer (embedding passes only), and the position its rotation is for
-// (the same as pos, but for the nodes of a tree: there the depth counts).
+// sequence's cache, and the position its rotation is for (the same, but for the nodes of a tree: there the depth counts).
 struct RowDesc {
-    int32_t seq, slot, pos, tok, rpos;
+    int32_t seq, slot, pos, rpos;
 };
 
 // Rows of one sequence inside a pass: consecutive rows, consecutive slots, consecutive positions.

@@ -52,7 +52,8 @@ __global__ void __launch_bounds__(CTL_THREADS) embed_kernel(const __grid_constan
     pdl_launch();
     pdl_wait();
     const RowDesc rd = a.plan.rows[blockIdx.x];
-    const int token = a.tok_src[rd.tok];
+    // a prompt's tokens lie by position, a round's by slot: [0] the next input, [1 + i] draft i
+    const int token = a.tok_src[a.tok_src == a.B.TOK ? rd.seq * (a.D.S + 1) + rd.slot : rd.pos];
     write_embedding(a, token, rd.seq, rd.slot);
 }
 

@@ -330,7 +330,7 @@ int plan_commit(del_ctx *c, const PlanBatch &b) {
 // rows of one pass: for every listed sequence `nrows` consecutive slots starting at slot0
 struct RowSpec { int seq, slot0, nrows; };
 
-void fill_plan(const del_ctx *c, PassPlan *p, const std::vector<RowSpec> &specs, bool prompt_tokens) {
+void fill_plan(const del_ctx *c, PassPlan *p, const std::vector<RowSpec> &specs) {
     memset(p, 0, sizeof(*p));
     int m = 0, ns = 0;
     for (const RowSpec &r : specs) {
@@ -338,7 +338,7 @@ void fill_plan(const del_ctx *c, PassPlan *p, const std::vector<RowSpec> &specs,
         p->seg[ns++] = Segment{r.seq, m, r.nrows, s.T + r.slot0};
         for (int i = 0; i < r.nrows; ++i) {
             const int slot = r.slot0 + i, pos = s.T + slot;
-            p->rows[m++] = RowDesc{r.seq, slot, pos, prompt_tokens ? pos : r.seq * (c->D.S + 1) + slot, pos};
+            p->rows[m++] = RowDesc{r.seq, slot, pos, pos};
         }
     }
     p->m = m;
@@ -599,21 +599,21 @@ std::vector<int> exit_layers(const std::vector<Job> &jobs) {
 void plan_draft_step(del_ctx *c, PlanBatch &pb, const std::vector<Job> &act, const std::vector<int> &Es, int i, DraftStep &st) {
     std::vector<RowSpec> full;
     for (const Job &j : act) full.push_back(RowSpec{j.seq, i, 1});
-    fill_plan(c, pb.add(&st.full_idx), full, false);
+    fill_plan(c, pb.add(&st.full_idx), full);
     for (size_t e = 0; e < Es.size(); ++e) {
         if (e == 0) { st.sub_idx.push_back(st.full_idx); continue; }
         std::vector<RowSpec> sub;
         for (const Job &j : act)
             if (j.E >= Es[e]) sub.push_back(RowSpec{j.seq, i, 1});
         int idx = -1;
-        if (!sub.empty()) fill_plan(c, pb.add(&idx), sub, false);
+        if (!sub.empty()) fill_plan(c, pb.add(&idx), sub);
         st.sub_idx.push_back(idx);
     }
     // sequences that sample: their drawn token is embedded as the next row by a launch of its own
     std::vector<RowSpec> smp;
     for (const Job &j : act)
         if (samples(c, j.seq)) smp.push_back(RowSpec{j.seq, i + 1, 1});
-    if (!smp.empty()) fill_plan(c, pb.add(&st.samp_idx), smp, false);
+    if (!smp.empty()) fill_plan(c, pb.add(&st.samp_idx), smp);
 }
 
 // layers 1..E of every drafting row, the exit head in one pass over W_lm, arg-max + confidence, next embedding
@@ -855,7 +855,7 @@ int enqueue_verify(del_ctx *c, const std::vector<Job> &jobs) {
             else specs.push_back(RowSpec{j.seq, 0, j.g + 1});
         }
         idx[k] = -1;
-        if (!specs.empty()) fill_plan(c, pb.add(&idx[k]), specs, false);
+        if (!specs.empty()) fill_plan(c, pb.add(&idx[k]), specs);
     }
     // sequences that drafted nothing still need their input token embedded
     int embed_idx = -1;
@@ -863,7 +863,7 @@ int enqueue_verify(del_ctx *c, const std::vector<Job> &jobs) {
         std::vector<RowSpec> specs;
         for (const Job &j : jobs)
             if (j.g == 0 && !j.stopped) specs.push_back(RowSpec{j.seq, 0, 1});
-        if (!specs.empty()) fill_plan(c, pb.add(&embed_idx), specs, false);
+        if (!specs.empty()) fill_plan(c, pb.add(&embed_idx), specs);
     }
     rc = plan_commit(c, pb);
     if (rc) return rc;
@@ -1290,7 +1290,7 @@ int del_prefill(del_ctx *c, int sq, const int32_t *prompt, int n_prompt, int max
         PlanBatch pb(c);
         int idx;
         s.T = ch.first;                      // rows are addressed relative to the committed length
-        fill_plan(c, pb.add(&idx), {RowSpec{sq, 0, ch.second}}, true);
+        fill_plan(c, pb.add(&idx), {RowSpec{sq, 0, ch.second}});
         rc = plan_commit(c, pb);
         if (rc) return rc;
         CtlArgs ca = ctl_base(c, idx);
@@ -1566,7 +1566,7 @@ int del_verify_tree(del_ctx *c, int sq, int n_drafts, const int32_t *tokens, con
     PlanBatch pb(c);
     int idx;
     PassPlan *p = pb.add(&idx);
-    fill_plan(c, p, {RowSpec{sq, 0, n}}, false);
+    fill_plan(c, p, {RowSpec{sq, 0, n}});
     for (int i = 0; i < n; ++i) p->rows[i].rpos = s.T + depth[i];
     rc = plan_commit(c, pb);
     if (rc) return rc;

@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(NW * 32, (NW == 8 && NT <= 4 ? 2 : 1)) rowgemm
         for (int cl = tid >> 4; cl < NR; cl += NTHREADS / 16) {
             const int c = row0 + cl;                // row of the pass; cl: its column in this launch
             const bool valid = c < m;
-            const RowDesc rd = valid ? plan->rows[c] : RowDesc{0, 0, 0, 0, 0};
+            const RowDesc rd = valid ? plan->rows[c] : RowDesc{0, 0, 0, 0};
             // product with the high parts + product with the low parts
             const float ra = HL ? res[cl * 16 + i] + res[(cl + NR) * 16 + i] : res[cl * 16 + i];
             // rows 8..15 of the tile at the same column (rotary partner / up row), read by threads i < 8 only
