@@ -19,12 +19,12 @@ namespace {
 // time where a destination page is only partly written).  So values are read by whole source pages: of contexts kept by halves, 5
 // bytes move where 4 would do.  The copies are asynchronous and one round ahead, page ids two rounds, positions three: a round would
 // otherwise wait for three to five round trips to memory in turn (2 x 4 003 of 8 001 positions, 1B shape: 165 us that way).
-constexpr int CP_WARPS = 4, CP_RUNS = 2;       // source pages of a destination page that are staged; what comes from further ones is loaded directly
+constexpr int CP_WARPS = 4, CP_RUNS = 2, CP_SPARSE = 4;      // source pages of a destination page that are staged, the next ones are loaded directly; with
+                                                             // more than CP_SPARSE, each token's values are loaded by themselves
 
 struct CompactArgs {
     PageView kv;
     del_compact c;
-    int32_t stages;            // 2; 1 where every part is a single round
 };
 
 // 16-bit element `slot` of a 32-byte row
@@ -36,7 +36,7 @@ __device__ __forceinline__ uint32_t pick(const uint4 (&r)[2], int slot) {
 }
 
 template <int HD> struct Compact {
-    static constexpr int K_BYTES = 16 * HD * 2, V_BYTES = HD * 32, STAGE = K_BYTES + CP_RUNS * V_BYTES;      // a warp's page of a round
+    static constexpr int K_BYTES = 16 * HD * 2, V_BYTES = HD * 32, STAGE = K_BYTES + CP_RUNS * V_BYTES, WARP = 2 * STAGE;      // a warp's page of a round; two rounds
 };
 
 template <int HD>
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const Compact
         f.src = sp >= 0 && sp < (int64_t)a.c.src_cols * 16 ? a.c.src_table[(size_t)b * a.c.src_stride + (sp >> 4)] : -1;
         f.slot = sp & 15;
     };
-    unsigned char *mine = smem + warp * a.stages * C::STAGE;
+    unsigned char *mine = smem + warp * C::WARP;
     auto fetch = [&](From &f, int stage) {                       // requests the round's keys and values
         if (!a.kv.holds(f.dst)) f.dst = -1;
         if (f.dst < 0 || !a.kv.holds(f.src)) f.src = -1;
@@ -78,7 +78,7 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const Compact
                 if (pg >= 0) cp_async16(ks + piece * 16, a.kv.k + (size_t)pg * page_elems + head + sl * HD + c, true);
             }
             uint32_t left = f.runs;
-            for (int r = 0; r < CP_RUNS && left; ++r, left &= left - 1) {
+            for (int r = 0; r < CP_RUNS && left && __popc(f.runs) <= CP_SPARSE; ++r, left &= left - 1) {
                 const int pg = __shfl_sync(0xffffffffu, f.src, __ffs(left) - 1);
                 const bf16 *v = a.kv.v + (size_t)pg * page_elems + head;
 #pragma unroll
@@ -105,7 +105,18 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const Compact
         __syncwarp();
         const unsigned char *ks = mine + stage * C::STAGE, *vs = ks + C::K_BYTES;
         uint32_t vals[DPL][8];
-        if (cur.moved) {
+        if (__popc(cur.runs) > CP_SPARSE) {
+            const uint16_t *v = reinterpret_cast<const uint16_t *>(a.kv.v) + head + (size_t)lane * 16;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const int pg = __shfl_sync(0xffffffffu, cur.src, j), sl = __shfl_sync(0xffffffffu, cur.slot, j);
+#pragma unroll
+                for (int d = 0; d < DPL; ++d) {
+                    const uint32_t x = pg >= 0 ? v[(size_t)pg * page_elems + d * 512 + sl] : 0u;
+                    vals[d][j >> 1] = j & 1 ? vals[d][j >> 1] | (x << 16) : x;
+                }
+            }
+        } else if (cur.moved) {
             uint4 rows[DPL][2];
             int run = -1;
 #pragma unroll
@@ -174,6 +185,60 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const Compact
         cur = nxt;
         nxt = later;
     }
+}
+
+// The same for a few pages, one round of one part (accepted paths): nothing to pipeline, and the tokens of a page come from several
+// others.  A lane loads its dimensions' values of each token by themselves, all on their way together.
+template <int HD>
+__global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_few_kernel(const CompactArgs a) {
+    constexpr int KV = HD / 16, DPL = HD / 32;                  // 16-byte pieces of 16 keys, dimensions, per lane
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.y;
+    const int n = min(max(a.c.counts[b], 0), a.c.max_count);
+    const int64_t start = a.c.dst_start[b], dp = (start >= 0 ? start >> 4 : -((-start + 15) >> 4)) + warp, i = dp * 16 + lane - start;
+    const size_t head = (size_t)blockIdx.x * a.kv.head_elems(), page_elems = a.kv.page_elems();
+    int dst = -1, src = -1, slot = 0;
+    if (dp >= 0 && dp < a.c.dst_cols && dp * 16 < start + n) {
+        const int sp = lane < 16 && i >= 0 && i < n ? a.c.src_pos[(size_t)b * a.c.pos_stride + i] : -1;
+        dst = a.c.dst_table[(size_t)b * a.c.dst_stride + dp];
+        if (sp >= 0 && sp < (int64_t)a.c.src_cols * 16) {
+            src = a.c.src_table[(size_t)b * a.c.src_stride + (sp >> 4)];
+            slot = sp & 15;
+        }
+        if (!a.kv.holds(dst) || !a.kv.holds(src)) src = -1;
+    }
+    const uint32_t moved = __ballot_sync(0xffffffffu, src >= 0);
+    uint4 keys[KV];
+    uint16_t vals[16][DPL];
+    if (moved) {
+#pragma unroll
+        for (int v = 0; v < KV; ++v) {
+            const int piece = v * 32 + lane, j = piece / (HD / 8), c = piece % (HD / 8) * 8;
+            const int pg = __shfl_sync(0xffffffffu, src, j), sl = __shfl_sync(0xffffffffu, slot, j);
+            if (pg >= 0) keys[v] = *reinterpret_cast<const uint4 *>(a.kv.k + (size_t)pg * page_elems + head + sl * HD + c);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int pg = __shfl_sync(0xffffffffu, src, j), sl = __shfl_sync(0xffffffffu, slot, j);
+            const uint16_t *v = reinterpret_cast<const uint16_t *>(a.kv.v) + (size_t)max(pg, 0) * page_elems + head + (size_t)lane * 16 + sl;
+            if (pg >= 0)
+#pragma unroll
+                for (int d = 0; d < DPL; ++d) vals[j][d] = v[d * 512];
+        }
+    }
+    __syncthreads();                                              // every page has been read
+    if (!moved) return;
+    bf16 *kd = a.kv.k + (size_t)dst * page_elems + head;
+    uint16_t *vd = reinterpret_cast<uint16_t *>(a.kv.v) + (size_t)dst * page_elems + head + (size_t)lane * 16;
+#pragma unroll
+    for (int v = 0; v < KV; ++v) {
+        const int piece = v * 32 + lane;
+        if ((moved >> (piece / (HD / 8))) & 1) *reinterpret_cast<uint4 *>(kd + piece * 8) = keys[v];
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if ((moved >> j) & 1)
+#pragma unroll
+            for (int d = 0; d < DPL; ++d) vd[d * 512 + j] = vals[j][d];
 }
 
 // ---------------------------------------------------------------- forks
@@ -331,7 +396,7 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
 }  // namespace
 
 cudaError_t launch_kv_compact(const PageView &kv, const del_compact &x, cudaStream_t st) {
-    CompactArgs a{kv, x, 0};
+    CompactArgs a{kv, x};
     // a warp for each destination page of a round; positions of up to max_count / 16 + 2 pages
     const int n_sms = current_sms(), pages = (x.max_count + 14) / 16 + 1, warps = pages < CP_WARPS ? pages : CP_WARPS;
     if (!n_sms) return cudaErrorInvalidDevice;
@@ -341,13 +406,17 @@ cudaError_t launch_kv_compact(const PageView &kv, const del_compact &x, cudaStre
         parts = (6 * n_sms + units - 1) / units;
         parts = parts < rounds ? parts : rounds;
     }
-    a.stages = (pages + parts - 1) / parts <= warps ? 1 : 2;
     const dim3 grid(a.kv.L * a.kv.nkv, x.batch, (unsigned)parts);
+    if (pages <= warps) {
+        if (a.kv.hd == 128) compact_few_kernel<128><<<grid, warps * 32, 0, st>>>(a);
+        else compact_few_kernel<64><<<grid, warps * 32, 0, st>>>(a);
+        return cudaGetLastError();
+    }
     static SmemAttrOnce attr128, attr64;
-    const cudaError_t e = a.kv.hd == 128 ? attr128.set(compact_kernel<128>, 2 * CP_WARPS * Compact<128>::STAGE) : attr64.set(compact_kernel<64>, 2 * CP_WARPS * Compact<64>::STAGE);
+    const cudaError_t e = a.kv.hd == 128 ? attr128.set(compact_kernel<128>, CP_WARPS * Compact<128>::WARP) : attr64.set(compact_kernel<64>, CP_WARPS * Compact<64>::WARP);
     if (e != cudaSuccess) return e;
-    if (a.kv.hd == 128) compact_kernel<128><<<grid, warps * 32, a.stages * warps * Compact<128>::STAGE, st>>>(a);
-    else compact_kernel<64><<<grid, warps * 32, a.stages * warps * Compact<64>::STAGE, st>>>(a);
+    if (a.kv.hd == 128) compact_kernel<128><<<grid, CP_WARPS * 32, CP_WARPS * Compact<128>::WARP, st>>>(a);
+    else compact_kernel<64><<<grid, CP_WARPS * 32, CP_WARPS * Compact<64>::WARP, st>>>(a);
     return cudaGetLastError();
 }
 
