@@ -514,7 +514,7 @@ def _refuse(what: str, why: str):
 
 def _vector(what: str, name: str, t, n: int, dev: int) -> int:
     """Address of a contiguous int32 vector of n entries on that device."""
-    if t.dtype is not _t.int32 or t.dim() != 1 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+    if t.dtype is not _t.int32 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
         _refuse(what, f"{name}: contiguous int32 [{n}] on the cache's device expected")
     return t.data_ptr()
 
@@ -525,7 +525,7 @@ def _table(what: str, name: str, t, rows: int, dev: int):
         _refuse(what, f"{name}: int32 [{rows}, columns] on the cache's device expected")
     n, cols = t.shape
     stride, one = t.stride()
-    if n != rows or cols < 1 or (cols > 1 and one != 1):
+    if n != rows or cols < 1 or (one != 1 and cols > 1):
         _refuse(what, f"{name}: int32 [{rows}, columns] with contiguous rows expected")
     return t.data_ptr(), cols, stride
 
@@ -537,7 +537,7 @@ def _pages(what: str, k, v):
         import torch
         _t = torch
     bf16, dev = _t.bfloat16, k.get_device()
-    if k.dtype is not bf16 or v.dtype is not bf16 or dev < 0 or v.get_device() != dev or k.dim() != 5:
+    if k.dtype is not bf16 or v.dtype is not bf16 or dev < 0 or v.get_device() != dev or k.dim() != 5 or v.dim() != 5:
         _refuse(what, "k_pages, v_pages: bf16 tensors of 5 dimensions on one CUDA device expected")
     n, layers, heads, slots, hd = k.shape
     if slots != 16 or v.shape != (n, layers, heads, hd, 16) or not (k.is_contiguous() and v.is_contiguous()):
@@ -547,8 +547,9 @@ def _pages(what: str, k, v):
 
 def _call(what: str, dev: int, fn, kv: bytes, args: bytes, stream):
     """The C call on the stream (None: the device's current one) with the device current; raises on an error code."""
-    st = stream.cuda_stream if stream is not None else _t._C._cuda_getCurrentRawStream(dev)
-    if _t._C._cuda_getDevice() == dev:
+    tc = _t._C
+    st = stream.cuda_stream if stream is not None else tc._cuda_getCurrentRawStream(dev)
+    if tc._cuda_getDevice() == dev:
         rc = fn(kv, args, st) if kv is not None else fn(args, st)
     else:
         with _t.cuda.device(dev):
@@ -597,7 +598,7 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
         mp = mask.data_ptr()
     a = _PACK_TREE(qp, op, lp, tp, _vector(what, "lens", lens, batch, dev), np_, mp, 0, q_seq, q_node, o_seq, o_node, batch, n, nh, layer,
                    cols, stride, max_len, scale or 0.0)
-    _call(what, dev, load_library().del_tree_attention, kv, a, stream)
+    _call(what, dev, (_lib or load_library()).del_tree_attention, kv, a, stream)
     return out
 
 
@@ -613,7 +614,7 @@ def kv_compact(k_pages, v_pages, src_table, src_pos, counts, dst_table, dst_star
     pp, most, p_stride = _table(what, "src_pos", src_pos, batch, dev)
     a = _PACK_COMPACT(sp, dp, pp, _vector(what, "counts", counts, batch, dev), _vector(what, "dst_start", dst_start, batch, dev), batch, most,
                       s_cols, s_stride, d_cols, d_stride, p_stride)
-    _call(what, dev, load_library().del_kv_compact, kv, a, stream)
+    _call(what, dev, (_lib or load_library()).del_kv_compact, kv, a, stream)
 
 
 def kv_fork(k_pages, v_pages, table, lens, parents, spare, n_spare, new_table, new_lens, counts, room: int = 0, free_pages=None, stream=None):
@@ -629,7 +630,7 @@ def kv_fork(k_pages, v_pages, table, lens, parents, spare, n_spare, new_table, n
                    _vector(what, "new_lens", new_lens, n_new, dev),
                    0 if free_pages is None else _vector(what, "free_pages", free_pages, n_pages, dev), _vector(what, "counts", counts, 2, dev),
                    n_old, n_new, cols, stride, new_cols, new_stride, n_listed, room)
-    _call(what, dev, load_library().del_kv_fork, kv, a, stream)
+    _call(what, dev, (_lib or load_library()).del_kv_fork, kv, a, stream)
 
 
 def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None, eos: int = 0, workspace=None, stream=None):
