@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;            // (l = 0: nothing is visible, the result is zero)
             const size_t out = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD;
-            if (n_splits > 1 && !half) *part_ml(q_sm, t * BQ + trow) = make_float2(m_ref, l);
+            if (n_splits > 1 && !half) *part_ml(q_sm, t * BQ + trow) = make_float2(m_ref, ok && !s_err ? l : NAN);
             float *po = reinterpret_cast<float *>(k_sm) + (size_t)(t * BQ + trow) * HD;
             for (int c0 = half * (HD / 2); c0 < (half + 1) * (HD / 2) && n_kb > 0; c0 += 32) {
                 uint32_t o[32];
@@ -524,44 +524,41 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     if (n_splits > 1) {
         cg::cluster_group cl = cg::this_cluster();
         cl.sync();
-        // Each CTA finishes a share of the rows: first the parts' weights, a thread per row; then the outputs, four columns per thread,
-        // all parts' loads on their way together.
-        constexpr int LPR = HD / 4, MAX_PARTS = 8;
+        // Each CTA finishes a share of the rows, four columns per thread, states and outputs of four parts on their way together (the
+        // states first and the weights through shared memory took a round trip more).
+        constexpr int LPR = HD / 4;
         const int parts = (nb + per - 1) / per, mine0 = rows * split / n_splits, mine1 = rows * (split + 1) / n_splits;     // (parts with blocks, this CTA's rows)
-        float *w_sm = reinterpret_cast<float *>(q_sm + TILES * BQ * 8);                          // [row][MAX_PARTS]
-        for (int x = mine0 + threadIdx.x; x < mine1; x += C::THREADS) {
-            float2 ml[MAX_PARTS];
-            bool failed = false;
-#pragma unroll
-            for (int k = 0; k < MAX_PARTS; ++k) {
-                ml[k] = k < parts ? *part_ml(cl.map_shared_rank(q_sm, k), x) : make_float2(-INFINITY, 0.f);
-                failed |= k < n_splits && *cl.map_shared_rank(const_cast<int *>(&s_err), k) != 0;
-            }
-            float M = -INFINITY, L = 0.f;
-#pragma unroll
-            for (int k = 0; k < MAX_PARTS; ++k) M = fmaxf(M, ml[k].x);
-            const float mu = M == -INFINITY ? 0.f : M;
-#pragma unroll
-            for (int k = 0; k < MAX_PARTS; ++k) { ml[k].x = ex2f(ml[k].x - mu); L += ml[k].y * ml[k].x; }
-            const float inv = failed ? NAN : L == 0.f ? 0.f : 1.f / L;
-#pragma unroll
-            for (int k = 0; k < MAX_PARTS; ++k) w_sm[x * MAX_PARTS + k] = ml[k].x * inv;
-        }
-        __syncthreads();
         for (int e = mine0 * LPR + threadIdx.x; e < mine1 * LPR; e += C::THREADS) {
             const int x = e / LPR, c = e % LPR;
             const size_t off = (size_t)x * HD + ((c ^ (x & 15)) << 2);
-            float4 v[MAX_PARTS];
-#pragma unroll
-            for (int k = 0; k < MAX_PARTS; ++k)
-                if (k < parts) v[k] = *reinterpret_cast<const float4 *>(cl.map_shared_rank(reinterpret_cast<float *>(k_sm), k) + off);
+            float M = -INFINITY, L = 0.f;
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int k0 = 0; k0 < parts; k0 += 4) {
+                float2 ml[4];
+                float4 v[4];
 #pragma unroll
-            for (int k = 0; k < MAX_PARTS; ++k)
-                if (k < parts) {
-                    const float w = w_sm[x * MAX_PARTS + k];
-                    o.x += v[k].x * w; o.y += v[k].y * w; o.z += v[k].z * w; o.w += v[k].w * w;
+                for (int k = 0; k < 4; ++k) {
+                    ml[k] = make_float2(-INFINITY, 0.f);
+                    if (k0 + k < parts) {
+                        ml[k] = *part_ml(cl.map_shared_rank(q_sm, k0 + k), x);
+                        v[k] = *reinterpret_cast<const float4 *>(cl.map_shared_rank(reinterpret_cast<float *>(k_sm), k0 + k) + off);
+                    }
                 }
+                const float m_new = fmaxf(fmaxf(M, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)), mu = m_new == -INFINITY ? 0.f : m_new;
+                const float f = ex2f(M - mu);
+                M = m_new;
+                L *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k0 + k < parts) {
+                        const float w = ex2f(ml[k].x - mu);
+                        L += ml[k].y * w;
+                        o.x += v[k].x * w; o.y += v[k].y * w; o.z += v[k].z * w; o.w += v[k].w * w;
+                    }
+            }
+            const float inv = L == 0.f ? 0.f : 1.f / L;             // (no number if a part gave up)
+            o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
             const int rr = row0 + x, i = node_of(rr), hq = rr - i * group;
             const size_t at = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD + 4 * c;
             uint2 hi, lo;
