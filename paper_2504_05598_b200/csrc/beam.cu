@@ -362,6 +362,10 @@ __device__ __forceinline__ void merge(const BeamArgs &a, int item, bool wait) {
     Shared &sm = shared();
     const int beams = a.b.beams, V = a.b.vocab, k = a.b.k, slices = a.slices, n_lists = beams * slices, n_cand = n_lists * k;
     const Cand cd(reinterpret_cast<unsigned char *>(&sm) + (sizeof(Shared) + 15) / 16 * 16, n_cand);
+    if (wait) {                            // (before the scores too: this kernel starts while the first one runs)
+        pdl_wait();
+        pdl_launch();
+    }
     double cum = 0.0;
     bool done = false;
     if ((int)threadIdx.x < beams) {
@@ -369,7 +373,6 @@ __device__ __forceinline__ void merge(const BeamArgs &a, int item, bool wait) {
         done = a.b.finished && a.b.finished[item * beams + threadIdx.x];
     }
     if (threadIdx.x == 0) sm.count[0] = 0;
-    if (wait) pdl_wait();
     const size_t list0 = (size_t)item * n_lists;
     for (int e = threadIdx.x; e < n_cand; e += THREADS) cd.key[e] = __ldcg(a.key + list0 * k + e);
     if ((int)threadIdx.x < beams) {
@@ -460,7 +463,8 @@ __global__ void __launch_bounds__(THREADS, 1) beam_slice_kernel(const BeamArgs a
     Shared &sm = shared();
     const int row = blockIdx.y, k = a.b.k, list = row * a.slices + blockIdx.x;
     const int lo = (int)min((int64_t)blockIdx.x * a.slice, (int64_t)a.b.vocab), hi = (int)min((int64_t)lo + a.slice, (int64_t)a.b.vocab);
-    if (!FUSED) pdl_launch();
+    pdl_wait();
+    pdl_launch();
     float m = -INFINITY;
     double s = 0.0;
     int count = 0;
@@ -481,10 +485,13 @@ cudaError_t launch(const BeamArgs &a, cudaStream_t st) {
     constexpr size_t fixed = (sizeof(Shared) + 15) / 16 * 16;
     const size_t merge_bytes = fixed + Cand::bytes(a.b.beams * a.slices * a.b.k);
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.blockDim = dim3(THREADS);
     cfg.stream = st;
     cfg.attrs = at;
+    cfg.numAttrs = 1;
     cfg.gridDim = dim3(a.slices, a.b.batch * a.b.beams);
     if (a.fused) {
         static SmemAttrOnce attr;
@@ -499,11 +506,11 @@ cudaError_t launch(const BeamArgs &a, cudaStream_t st) {
             if (e != cudaSuccess) return e;
             if (dev < DEL_MAX_DEVICES) big[dev] = true;
         }
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = a.slices;
-        at[0].val.clusterDim.y = a.b.beams;
-        at[0].val.clusterDim.z = 1;
-        cfg.numAttrs = 1;
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = a.slices;
+        at[1].val.clusterDim.y = a.b.beams;
+        at[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
         cfg.dynamicSmemBytes = merge_bytes;
         return cudaLaunchKernelEx(&cfg, kern, a);
     }
@@ -516,9 +523,6 @@ cudaError_t launch(const BeamArgs &a, cudaStream_t st) {
     // (the second kernel's CTAs are few and short: they start while the first drains, and wait for its end before they read)
     cfg.gridDim = dim3(a.b.batch);
     cfg.dynamicSmemBytes = merge_bytes;
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, beam_merge_kernel, a);
 }
 

@@ -45,6 +45,7 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const Compact
     extern __shared__ __align__(16) unsigned char smem[];
     constexpr int DPL = HD / 32;                                // dimensions per lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n_warps = blockDim.x >> 5, b = blockIdx.y;
+    pdl_wait();
     const int n = min(max(a.c.counts[b], 0), a.c.max_count);
     const int64_t start = a.c.dst_start[b], first_page = start >= 0 ? start >> 4 : -((-start + 15) >> 4);
     const int64_t all_pages = n > 0 ? ((start + n - 1) >> 4) - first_page + 1 : 0;
@@ -193,6 +194,7 @@ template <int HD>
 __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_few_kernel(const CompactArgs a) {
     constexpr int KV = HD / 16, DPL = HD / 32;                  // 16-byte pieces of 16 keys, dimensions, per lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.y;
+    pdl_wait();
     const int n = min(max(a.c.counts[b], 0), a.c.max_count);
     const int64_t start = a.c.dst_start[b], dp = (start >= 0 ? start >> 4 : -((-start + 15) >> 4)) + warp, i = dp * 16 + lane - start;
     const size_t head = (size_t)blockIdx.x * a.kv.head_elems(), page_elems = a.kv.page_elems();
@@ -286,6 +288,7 @@ __global__ void __launch_bounds__(FK_THREADS) fork_kernel(const ForkArgs a) {
     const int r = threadIdx.x, n_cta = gridDim.x;
     first[r] = INT32_MAX;
     __syncthreads();
+    pdl_wait();
     int parent = -1, len = 0;
     if (r < f.n_new) {
         parent = f.parents[r];
@@ -408,16 +411,13 @@ cudaError_t launch_kv_compact(const PageView &kv, const del_compact &x, cudaStre
     }
     const dim3 grid(a.kv.L * a.kv.nkv, x.batch, (unsigned)parts);
     if (pages <= warps) {
-        if (a.kv.hd == 128) compact_few_kernel<128><<<grid, warps * 32, 0, st>>>(a);
-        else compact_few_kernel<64><<<grid, warps * 32, 0, st>>>(a);
-        return cudaGetLastError();
+        return a.kv.hd == 128 ? launch_cluster(compact_few_kernel<128>, grid, warps * 32, 0, 1, st, a) : launch_cluster(compact_few_kernel<64>, grid, warps * 32, 0, 1, st, a);
     }
     static SmemAttrOnce attr128, attr64;
     const cudaError_t e = a.kv.hd == 128 ? attr128.set(compact_kernel<128>, CP_WARPS * Compact<128>::WARP) : attr64.set(compact_kernel<64>, CP_WARPS * Compact<64>::WARP);
     if (e != cudaSuccess) return e;
-    if (a.kv.hd == 128) compact_kernel<128><<<grid, CP_WARPS * 32, CP_WARPS * Compact<128>::WARP, st>>>(a);
-    else compact_kernel<64><<<grid, CP_WARPS * 32, CP_WARPS * Compact<64>::WARP, st>>>(a);
-    return cudaGetLastError();
+    return a.kv.hd == 128 ? launch_cluster(compact_kernel<128>, grid, CP_WARPS * 32, CP_WARPS * Compact<128>::WARP, 1, st, a)
+                          : launch_cluster(compact_kernel<64>, grid, CP_WARPS * 32, CP_WARPS * Compact<64>::WARP, 1, st, a);
 }
 
 extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *cuda_stream) {
@@ -451,6 +451,5 @@ extern "C" int del_kv_fork(const del_pages *kv, const del_fork_args *x, void *cu
     static SmemAttrOnce attr;
     const size_t bits = x->free_pages ? ((size_t)a.kv.n_pages + 31) / 32 * 4 : 0;
     if (attr.set(fork_kernel, FK_MAX_FREE / 8) != cudaSuccess) return DEL_ECUDA;
-    fork_kernel<<<n_sms, FK_THREADS, bits, (cudaStream_t)cuda_stream>>>(a);
-    return cudaGetLastError() == cudaSuccess ? DEL_OK : DEL_ECUDA;
+    return launch_cluster(fork_kernel, dim3(n_sms), FK_THREADS, bits, 1, (cudaStream_t)cuda_stream, a) == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }

@@ -38,6 +38,10 @@ inline int current_sms() {
     return sms;
 }
 
+// A launch of these operators: clusters of cluster_x CTAs, and programmatic dependent launch, so that the launch itself runs beside
+// the kernel before it (0.3 to 0.6 us of a small call, 1 to 2 us of a large one).  Every kernel waits (pdl_wait) before it touches global memory, and lets the next one
+// start (pdl_launch) only after that, so that a kernel that runs beside this one finds the work of all kernels before this one done.
+// A kernel that writes pages never lets the next one start before its end: the decode attention reads committed pages before it waits.
 template <typename K, typename... A>
 inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, int cluster_x, cudaStream_t st, const A &...args) {
     cudaLaunchConfig_t cfg = {};
@@ -45,12 +49,14 @@ inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, i
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster_x;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster_x;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = cluster_x > 1 ? 1 : 0;
+    cfg.numAttrs = cluster_x > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 

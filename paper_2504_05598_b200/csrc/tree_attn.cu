@@ -36,6 +36,8 @@ __global__ void __launch_bounds__(THREADS, HD == 64 ? 2 : 1) tree_attention_kern
     __shared__ float2 tile_ml[16];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int n_splits = gridDim.x, split = blockIdx.x;
+    pdl_wait();
+    pdl_launch();
     const int group = a.nh / a.kv.nkv, n_mt = (a.max_nodes * group + 15) >> 4;
     const int kvh = blockIdx.y / n_mt, mt = blockIdx.y - kvh * n_mt, b = blockIdx.z;
     // page ids: lane i holds the id of the warp's i-th page of the current 32

@@ -139,6 +139,11 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n_splits = gridDim.x, split = blockIdx.x, b = blockIdx.z;
     const int group = a.nh / a.kv.nkv;
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
+    }
+    pdl_wait();                                                     // (before tensor memory is taken: the kernel before this one may still want some)
     const int n_rt = (a.max_nodes * group + TILES * BQ - 1) / (TILES * BQ);
     const int kvh = blockIdx.y / n_rt, row0 = (blockIdx.y - kvh * n_rt) * TILES * BQ;
     const float inv_group = 1.f / (float)group;
@@ -158,9 +163,6 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             const int u = e * 256 + t_tid, rr = row0 + t_of * BQ + u / PPR;
             q_pre[e] = rr < a.max_nodes * group ? *reinterpret_cast<const uint4 *>(q_row(rr) + u % PPR * 8) : make_uint4(0, 0, 0, 0);
         }
-    } else if (warp == 0 && lane == 0) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.k) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.v) : "memory");
     }
     const tree::Seq s = tree::load_seq(a, b);
     const int R = s.n * group;
@@ -208,6 +210,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = tmem_base_s;
+    pdl_launch();
 
     if (warp == 0) {
         int n_k = 0, n_v = 0;                        // blocks whose keys, whose values are on their way
