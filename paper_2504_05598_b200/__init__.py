@@ -573,7 +573,7 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
 
     q: bf16 [batch, nodes, heads, head_dim], the last two dimensions contiguous; page_table int32 [batch, columns]; lens, nodes int32
     [batch]; mask int64 [batch, nodes] (bit j of entry i: node i sees node j; None: a chain).  out (and out_lo, the low part of the result)
-    like q, made when None; returns out.  max_len: what lens are expected to reach."""
+    like q, made when None (on `stream`, whose work comes before any use of it); returns out.  max_len: what lens are expected to reach."""
     what = "del_tree_attention"
     kv, _, hd, dev = _pages(what, k_pages, v_pages)
     shape = q.shape
@@ -581,7 +581,8 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
         _refuse(what, "q: [batch, nodes, heads, head_dim] expected")
     batch, n, nh, _ = shape
     if out is None:
-        out = _t.zeros(shape, dtype=_t.bfloat16, device=k_pages.device)
+        with _t.cuda.stream(stream):
+            out = _t.zeros(shape, dtype=_t.bfloat16, device=k_pages.device)
     qp, q_seq, q_node = _rows_of_heads(what, "q", q, shape, dev)
     op, o_seq, o_node = _rows_of_heads(what, "out", out, shape, dev)
     lp = np_ = mp = 0
@@ -669,9 +670,12 @@ def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None,
     head = (logits.data_ptr(), scores.data_ptr(), fp, out_scores.data_ptr(), out_tokens.data_ptr(), out_rows.data_ptr())
     tail = (row, batch, beams, vocab, out[1], eos, dtype)
     if workspace is None:
-        workspace = _t.empty(lib.del_beam_workspace_bytes(_PACK_BEAM(*head, 0, 0, *tail)), dtype=_t.uint8, device=logits.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        n = lib.del_beam_workspace_bytes(_PACK_BEAM(*head, 0, 0, *tail))
+        if stream is None:
+            workspace = _t.empty(n, dtype=_t.uint8, device=logits.device)
+        else:                    # (memory that the current stream gave back may still be in use there)
+            with _t.cuda.stream(stream):
+                workspace = _t.empty(n, dtype=_t.uint8, device=logits.device)
     elif workspace.dtype is not _t.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse(what, "workspace: contiguous uint8 on the logits' device expected")
     _call(what, dev, lib.del_beam_select, None, _PACK_BEAM(*head, workspace.data_ptr(), workspace.numel(), *tail), stream)

@@ -381,12 +381,40 @@ def test_calls_on_streams_and_in_graphs():
                 graph.replay()
         third = torch.cuda.Stream()
         eager = torch.zeros_like(q)
+        third.wait_stream(torch.cuda.current_stream())
         dl.tree_attention(q, k, v, 2, table, lens, nodes, m, out=eager, stream=third)
         torch.cuda.synchronize()
         want = br.beam_ref(logits.cpu(), scores.cpu(), 4)
         for o, b in outs:
             assert torch.equal(o, eager)
             assert np.array_equal(b[1].cpu().numpy(), want[1]) and np.array_equal(b[2].cpu().numpy(), want[2])
+
+
+def test_what_a_call_makes_belongs_to_its_stream():
+    """A call on another stream than the busy current one: its output is not cleared by work of the current stream that comes late,
+    and its workspace is no memory that the current stream still reads."""
+    q, k, v, table, lens, nodes, m = [dev(t) for t in make_tree(4, 2, 64, [100], [5], 5, seed=8)]
+    logits, scores = torch.randn(1, 4, 5000, device="cuda"), torch.zeros(1, 4, device="cuda")
+    outs, want = [[torch.zeros(1, 4, dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)] for _ in range(2)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                                 # loads the kernels
+        att = dl.tree_attention(q, k, v, 1, table, lens, nodes, m)
+        dl.beam_select(logits, scores, *want)
+    torch.cuda.synchronize()
+    shape = dl.BeamC(*(dict(batch=1, beams=4, vocab=5000, k=4, dtype=0, row_stride=5000).get(n, 0) for n, _ in dl.BeamC._fields_))
+    n = dl.load_library().del_beam_workspace_bytes(dl.C.byref(shape))
+    held = torch.full((n,), 77, dtype=torch.uint8, device="cuda")
+    seen = torch.zeros_like(held)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)                                # the current stream is busy for some 50 ms
+    seen.copy_(held)
+    del held
+    got = dl.tree_attention(q, k, v, 1, table, lens, nodes, m, stream=side)
+    dl.beam_select(logits, scores, *outs, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got, att)
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    assert (seen == 77).all()
 
 
 def test_beam_search_over_shared_pages():
