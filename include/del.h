@@ -384,7 +384,7 @@ int del_tree_attention(const del_pages *kv, const del_tree_attn *args, void *cud
  * dst_table the same pointer) a row's sources and destinations may overlap if src_pos[b] ascends strictly and src_pos[b][i] >=
  * dst_start[b] + i; otherwise no position written may be one that is read.  No position may be written twice.  A position outside its table
  * (src_cols * 16, dst_cols * 16) or on a
- * page id outside [0, n_pages) is not moved. */
+ * page id outside [0, n_pages) is not moved.  batch 1..65535, max_count 1..2^30. */
 typedef struct {
     const int32_t *src_table, *dst_table;    /* [batch] rows of src_cols / dst_cols entries, src_stride / dst_stride apart */
     const int32_t *src_pos;                  /* [batch][max_count], rows pos_stride apart */
@@ -402,7 +402,8 @@ int del_kv_compact(const del_pages *kv, const del_compact *args, void *cuda_stre
  *     id is outside [0, n_pages), the entry becomes -1 and counts[1] goes up by one;
  *   - free_pages (may be null): the ids in [0, n_pages) that no new row holds, ascending, counts[0] of them, the rest of the array
  *     left as it was; it holds n_pages entries, may not overlap spare, and serves as the next call's spare with n_spare = counts.
- * 1 <= n_old, n_new <= 1024; with free_pages n_pages <= 1 << 20. */
+ *   - lens below 0 count as 0, and are cut to what the rows of both tables hold; shared entries are passed on as they are.
+ * 1 <= n_old, n_new <= 1024; n_new * new_cols < 2^31; with free_pages n_pages <= 1 << 20. */
 typedef struct {
     const int32_t *table, *lens, *parents;   /* [n_old] rows of old_cols entries old_stride apart, [n_old], [n_new] */
     const int32_t *spare, *n_spare;

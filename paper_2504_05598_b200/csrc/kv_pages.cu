@@ -425,7 +425,7 @@ extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *c
     if (!x || !page_view(kv, &view)) return DEL_EINVAL;
     if (!x->src_table || !x->dst_table || !x->src_pos || !x->counts || !x->dst_start) return DEL_EINVAL;
     if (((uintptr_t)x->src_table | (uintptr_t)x->dst_table | (uintptr_t)x->src_pos | (uintptr_t)x->counts | (uintptr_t)x->dst_start) & 3) return DEL_EINVAL;
-    if (x->batch < 1 || x->batch > 65535 || x->max_count < 1 || x->src_cols < 1 || x->dst_cols < 1) return DEL_EINVAL;
+    if (x->batch < 1 || x->batch > 65535 || x->max_count < 1 || x->max_count > (1 << 30) || x->src_cols < 1 || x->dst_cols < 1) return DEL_EINVAL;
     if (x->src_stride < 0 || x->dst_stride < 0 || x->pos_stride < 0) return DEL_EINVAL;
     return launch_kv_compact(view, *x, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }
@@ -439,6 +439,7 @@ extern "C" int del_kv_fork(const del_pages *kv, const del_fork_args *x, void *cu
         return DEL_EINVAL;
     if (x->n_old < 1 || x->n_old > FK_ROWS || x->n_new < 1 || x->n_new > FK_ROWS) return DEL_EINVAL;
     if (x->old_cols < 1 || x->new_cols < 1 || x->old_cols > INT32_MAX / 16 || x->new_cols > INT32_MAX / 16) return DEL_EINVAL;
+    if ((int64_t)x->n_new * x->new_cols > INT32_MAX) return DEL_EINVAL;               // spare pages are counted in 32 bits
     if (x->old_stride < x->old_cols || x->new_stride < x->new_cols || x->spare_cap < 0 || x->room < 0) return DEL_EINVAL;
     if (x->free_pages && a.kv.n_pages > FK_MAX_FREE) return DEL_EINVAL;
     const size_t old_bytes = 4 * ((size_t)(x->n_old - 1) * x->old_stride + x->old_cols), new_bytes = 4 * ((size_t)(x->n_new - 1) * x->new_stride + x->new_cols);

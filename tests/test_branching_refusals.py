@@ -80,6 +80,12 @@ def test_caches_that_are_refused(over):
     assert call("del_kv_fork", dl.ForkC, FORK, {}, over) == dl.EINVAL
 
 
+def test_sizes_that_counts_of_32_bits_do_not_hold():
+    assert call("del_kv_compact", dl.CompactC, COMPACT, dict(max_count=(1 << 31) - 1, pos_stride=(1 << 31) - 1)) == dl.EINVAL
+    far = dict(table=1 << 40, lens=1 << 41, new_table=1 << 42, new_lens=1 << 43)
+    assert call("del_kv_fork", dl.ForkC, FORK, dict(far, n_new=1024, new_cols=1 << 21, new_stride=1 << 21, room=(1 << 31) - 1)) == dl.EINVAL
+
+
 def test_null_structs():
     lib, pages = dl.load_library(), kv()
     for name in ("del_tree_attention", "del_kv_compact", "del_kv_fork"):
