@@ -350,6 +350,76 @@ def test_beam_select_strides():
         check_beam(view, torch.zeros(2, 3), 9)
 
 
+def test_beam_select_with_a_workspace():
+    """A workspace that is handed in: whatever it holds, the same results; one byte too few is refused."""
+    g = torch.Generator().manual_seed(9)
+    for batch, beams, vocab, k in [(1, 4, 3001, 4), (30, 5, 20011, 9)]:
+        logits, scores = torch.randn(batch, beams, vocab, generator=g), torch.zeros(batch, beams)
+        want = check_beam(logits, scores, k)
+        shape = dl.BeamC(*(dict(batch=batch, beams=beams, vocab=vocab, k=k, dtype=0, row_stride=vocab).get(n, 0) for n, _ in dl.BeamC._fields_))
+        size = dl.load_library().del_beam_workspace_bytes(dl.C.byref(shape))
+        outs = [torch.zeros_like(t) for t in want]
+        for fill in (0, 255, 127):
+            work = torch.full((size,), fill, dtype=torch.uint8, device="cuda")
+            dl.beam_select(logits.cuda(), scores.cuda(), *outs, workspace=work)
+            assert all(torch.equal(a, b) for a, b in zip(outs, want))
+        with pytest.raises(dl.DelError) as e:
+            dl.beam_select(logits.cuda(), scores.cuda(), *outs, workspace=work[:-1])
+        assert e.value.code == dl.ENOSPC
+
+
+# ---------------------------------------------------------------- offsets that 32 bits do not hold
+def test_caches_of_more_than_2_32_elements():
+    """Pages at the far end of a large cache attended (both forms), compacted and forked; the few pages in use are checked against the
+    same calls' plain forms on a small cache."""
+    n_pages, layers, nkv, hd = 8300, 32, 8, 128                    # 4.35e9 keys
+    small_k, small_v = br.pool(12, layers, nkv, hd, 5)
+    far = torch.tensor([8299, 8210, 8193, 8298, 8250, 8201, 8297, 8222, 4097, 8290, 2, 8233])      # page i of the small cache lies here
+    k = torch.empty(n_pages, layers, nkv, 16, hd, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty(n_pages, layers, nkv, hd, 16, dtype=torch.bfloat16, device="cuda")
+    assert k.numel() > 2 ** 32
+
+    def put():
+        k[far.cuda()], v[far.cuda()] = small_k.cuda(), small_v.cuda()
+
+    def same():
+        return torch.equal(k[far.cuda()].cpu(), small_k) and torch.equal(v[far.cuda()].cpu(), small_v)
+
+    put()
+    i32 = dict(dtype=torch.int32)
+    near = torch.tensor([[0, 3, 6, 9], [1, 2, 4, 10]], **i32)
+    table = far[near.long()].to(torch.int32)
+    lens, nodes, mask = torch.tensor([41, 17], **i32), torch.tensor([9, 5], **i32), br.random_masks(2, 9, 3)
+    q = torch.randn(2, 9, 32, hd, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    ref, mass, dots = br.tree_attention_ref(q, small_k, small_v, layers, near, lens, nodes, mask)
+    bound = br.tree_attention_bound(ref, mass, dots, hd, 64)
+    wide = torch.full((2, 4096), 0x7ffffff0, **i32)
+    wide[:, :4] = table
+    for t in (table, wide):
+        got = dl.tree_attention(q.cuda(), k, v, layers, t.cuda(), lens.cuda(), nodes.cuda(), mask.cuda()).cpu().double()
+        live = ~ref.isnan()
+        assert ((got - ref).abs() <= bound)[live].all()
+    # in place (few pages), and from one row's pages into others
+    pos = torch.tensor([[43, 45, 46], [18, 20, 21]], **i32)
+    table_d = table.cuda()
+    dl.kv_compact(k, v, table_d, pos.cuda(), torch.tensor([3, 2], **i32).cuda(), table_d, lens.cuda())
+    br.compact_ref(small_k, small_v, near, pos, torch.tensor([3, 2], **i32), near, lens)
+    assert same()
+    src = torch.tensor([[i for i in range(0, 41, 2)] + [0] * 60], **i32)
+    out_near = torch.tensor([[11, 8, 7, 5, 5, 5]], **i32)
+    out_near[0, 4:] = -1
+    dl.kv_compact(k, v, table_d[:1], src.cuda(), torch.tensor([21], **i32).cuda(), torch.where(out_near >= 0, far[out_near.long()].to(torch.int32), out_near).cuda(),
+                  torch.tensor([16], **i32).cuda())
+    br.compact_ref(small_k, small_v, near[:1], src, torch.tensor([21], **i32), out_near, torch.tensor([16], **i32))
+    assert same()
+    # a fork copies a part-filled page between far pages
+    new, new_lens, counts = torch.full((3, 5), -1, **i32).cuda(), torch.zeros(3, **i32).cuda(), torch.zeros(2, **i32).cuda()
+    dl.kv_fork(k, v, table_d, lens.cuda(), torch.tensor([1, 0, 0], **i32).cuda(), far[[11, 8]].to(torch.int32).cuda(), torch.tensor([2], **i32).cuda(), new, new_lens, counts)
+    assert new[2].tolist() == [8299, 8298, 8233, -1, -1] and counts.tolist() == [0, 0]
+    small_k[11], small_v[11] = small_k[6], small_v[6]
+    assert same()
+
+
 # ---------------------------------------------------------------- streams, graphs, several calls at once
 def test_calls_on_streams_and_in_graphs():
     """Each operator captured twice into graphs that are replayed interleaved, on changed inputs, beside an eager call on a third stream."""
@@ -415,6 +485,64 @@ def test_what_a_call_makes_belongs_to_its_stream():
     assert torch.equal(got, att)
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
     assert (seen == 77).all()
+
+
+@pytest.mark.parametrize("vocab,beams", [(700, 4), (40000, 12)])      # selection in one launch, in two
+def test_calls_in_a_row_are_calls_one_by_one(vocab, beams):
+    """Steps of selection, fork, compaction and attention that feed one another without a wait on the host, and replayed from a graph,
+    give what they give when the host waits after each call: no kernel reads before the one before it has written."""
+    nh, nkv, hd, cols, steps, n_pages = 8, 2, 64, 12, 10, 400
+    i32 = dict(dtype=torch.int32, device="cuda")
+    g = torch.Generator().manual_seed(beams)
+    k0, v0 = br.pool(n_pages, 3, nkv, hd, 2, "cuda")
+    logits = [torch.randn(1, beams, vocab, generator=g).cuda() for _ in range(steps)]
+    q = [torch.randn(beams, 3, nh, hd, generator=g).to(torch.bfloat16).cuda() for _ in range(steps)]
+    order = torch.randperm(n_pages, generator=g).to(torch.int32)
+    keep = (1 + 2 * torch.arange(60)).to(torch.int32).repeat(beams, 1).cuda()
+    n_keep, zero, page_ids = torch.full((beams,), 40, **i32), torch.zeros(beams, **i32), order[:beams * 8].view(beams, 8).contiguous().cuda()
+    other = order[beams * 8: beams * 11].view(beams, 3).contiguous().cuda()
+    spare = order[beams * 11:].cuda()
+    spares, n_spare = [spare[i * beams:(i + 1) * beams] for i in range(steps)], torch.tensor([beams], **i32)
+
+    class State:
+        def __init__(self):
+            self.k, self.v = k0.clone(), v0.clone()
+            self.tables = [torch.zeros(beams, cols, **i32) for _ in range(steps + 1)]
+            self.tables[0][:, :8] = page_ids
+            self.lens = [torch.full((beams,), 97, **i32) if i == 0 else torch.zeros(beams, **i32) for i in range(steps + 1)]
+            self.scores = [torch.zeros(1, beams, device="cuda") for _ in range(steps + 1)]
+            self.tokens, self.rows = ([torch.zeros(1, beams, **i32) for _ in range(steps)] for _ in range(2))
+            self.counts = [torch.zeros(2, **i32) for _ in range(steps)]
+            self.out = [torch.zeros_like(x) for x in q]
+
+        def run(self, wait):
+            for i in range(steps):
+                for call in (lambda: dl.beam_select(logits[i], self.scores[i], self.scores[i + 1], self.tokens[i], self.rows[i]),
+                             lambda: dl.kv_fork(self.k, self.v, self.tables[i], self.lens[i], self.rows[i].view(-1), spares[i], n_spare, self.tables[i + 1],
+                                                self.lens[i + 1], self.counts[i], room=3),
+                             lambda: dl.kv_compact(self.k, self.v, self.tables[i + 1], keep, n_keep, other, zero),
+                             lambda: dl.tree_attention(q[i], self.k, self.v, 1 + i % 3, self.tables[i + 1], self.lens[i + 1], out=self.out[i]),
+                             lambda: dl.kv_compact(self.k, self.v, self.tables[i + 1], keep[:, 30:35], n_keep, self.tables[i + 1], self.lens[i + 1])):
+                    call()
+                    if wait:
+                        torch.cuda.synchronize()
+
+        def all(self):
+            return [self.k, self.v, *self.tables[1:], *self.lens[1:], *self.scores[1:], *self.tokens, *self.rows, *self.counts, *self.out]
+
+    one, row, graphed = State(), State(), State()
+    torch.cuda.synchronize()
+    one.run(True)
+    row.run(False)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        graphed.run(False)
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b, c in zip(one.all(), row.all(), graphed.all()):
+        assert torch.equal(a, b) and torch.equal(a, c)
+    assert not torch.equal(one.k, k0)
 
 
 def test_beam_search_over_shared_pages():
