@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct as _struct
+from functools import lru_cache as _lru_cache
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -634,6 +635,11 @@ def kv_fork(k_pages, v_pages, table, lens, parents, spare, n_spare, new_table, n
     _call(what, dev, (_lib or load_library()).del_kv_fork, kv, a, stream)
 
 
+@_lru_cache(maxsize=256)
+def _beam_workspace(batch: int, beams: int, vocab: int, k: int) -> int:
+    return load_library().del_beam_workspace_bytes(_PACK_BEAM(0, 0, 0, 0, 0, 0, 0, 0, vocab, batch, beams, vocab, k, 0, 0))
+
+
 def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None, eos: int = 0, workspace=None, stream=None):
     """del_beam_select: the k best continuations of every item, k = out_scores.shape[1].
 
@@ -666,11 +672,10 @@ def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None,
     for t in (out_tokens, out_rows):
         if t.shape != out or t.dtype is not _t.int32 or t.get_device() != dev or not t.is_contiguous():
             _refuse(what, "out_tokens, out_rows: contiguous int32 [batch, k] on the logits' device expected")
-    lib = load_library()
     head = (logits.data_ptr(), scores.data_ptr(), fp, out_scores.data_ptr(), out_tokens.data_ptr(), out_rows.data_ptr())
     tail = (row, batch, beams, vocab, out[1], eos, dtype)
     if workspace is None:
-        n = lib.del_beam_workspace_bytes(_PACK_BEAM(*head, 0, 0, *tail))
+        n = _beam_workspace(batch, beams, vocab, out[1])
         if stream is None:
             workspace = _t.empty(n, dtype=_t.uint8, device=logits.device)
         else:                    # (memory that the current stream gave back may still be in use there)
@@ -678,4 +683,4 @@ def beam_select(logits, scores, out_scores, out_tokens, out_rows, finished=None,
                 workspace = _t.empty(n, dtype=_t.uint8, device=logits.device)
     elif workspace.dtype is not _t.uint8 or workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse(what, "workspace: contiguous uint8 on the logits' device expected")
-    _call(what, dev, lib.del_beam_select, None, _PACK_BEAM(*head, workspace.data_ptr(), workspace.numel(), *tail), stream)
+    _call(what, dev, (_lib or load_library()).del_beam_select, None, _PACK_BEAM(*head, workspace.data_ptr(), workspace.numel(), *tail), stream)
