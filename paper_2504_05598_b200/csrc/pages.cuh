@@ -39,9 +39,10 @@ inline int current_sms() {
 }
 
 // A launch of these operators: clusters of cluster_x CTAs, and programmatic dependent launch, so that the launch itself runs beside
-// the kernel before it (0.3 to 0.6 us of a small call, 1 to 2 us of a large one).  Every kernel waits (pdl_wait) before it touches global memory, and lets the next one
-// start (pdl_launch) only after that, so that a kernel that runs beside this one finds the work of all kernels before this one done.
-// A kernel that writes pages never lets the next one start before its end: the decode attention reads committed pages before it waits.
+// the kernel before it (0.3 to 0.6 us of a small call, 1 to 2 us of a large one).  Every kernel waits (pdl_wait) before it touches
+// global memory, and lets the next one start (pdl_launch) only after that, so that a kernel that runs beside this one finds the work of
+// all kernels before this one done.  A kernel that writes pages never lets the next one start before its end: the decode attention reads
+// committed pages before it waits.
 template <typename K, typename... A>
 inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, int cluster_x, cudaStream_t st, const A &...args) {
     cudaLaunchConfig_t cfg = {};
@@ -64,10 +65,18 @@ inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, i
 // `kept`: the caller's record per kernel).  A launch of more runs in waves: of clusters of 8 with one CTA per SM, B200 holds 15.
 struct ClusterRoom {
     int n[DEL_MAX_DEVICES][17] = {};
+    bool wide[DEL_MAX_DEVICES] = {};       // clusters of more than 8 are allowed for the kernel
     template <typename K> int of(K kern, int threads, size_t smem, int cluster_x) {
         int dev = 0;
         if (cluster_x < 1 || cluster_x > 16 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEL_MAX_DEVICES) return 0;
         if (n[dev][cluster_x]) return n[dev][cluster_x];
+        if (cluster_x > 8 && !wide[dev]) {
+            if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+                cudaGetLastError();
+                return 0;
+            }
+            wide[dev] = true;
+        }
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(cluster_x);
         cfg.blockDim = dim3(threads);
@@ -85,10 +94,15 @@ struct ClusterRoom {
         }
         return n[dev][cluster_x] = got;
     }
-    // the largest cluster size up to `most` (1: none) of which `units` are resident together
-    template <typename K> int best(K kern, int threads, size_t smem, int64_t units, int most) {
-        for (int c = most < 8 ? most : 8; c > 1; --c)
-            if (units <= of(kern, threads, smem, c)) return c;
+    // Cluster size (1: none) for `units` clusters with `steps` steps of work each: of those sizes whose clusters are all resident
+    // together the one with the fewest steps per CTA, of equal ones the smallest.  Beyond 8 it pays where steps are many (one sequence of 30 000
+    // positions, 8B shape: 10 CTAs per kv head 36.8 us, 8 CTAs 42.4; 1B shape 16 CTAs 22.9, 8 CTAs 35.3).
+    template <typename K> int best(K kern, int threads, size_t smem, int64_t units, int steps) {
+        for (int c = steps < 16 ? steps : 16; c > 1; --c)
+            if (units <= of(kern, threads, smem, c)) {
+                const int each = (steps + c - 1) / c;
+                return (steps + each - 1) / each;
+            }
         return 1;
     }
 };

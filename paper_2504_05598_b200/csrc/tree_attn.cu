@@ -73,9 +73,19 @@ __global__ void __launch_bounds__(THREADS, HD == 64 ? 2 : 1) tree_attention_kern
     const int n_pages = (s.n_keys + 15) >> 4;
     const size_t page_stride = a.kv.page_elems(), head_off = ((size_t)(a.layer - 1) * a.kv.nkv + kvh) * a.kv.head_elems();
     const int key0 = 4 * (g >> 1) + (g & 1);                    // token of column g of score tile 0; tile 1: +2
+    // With one CTA per SM the warps' own loads do not cover the latency: the next page is requested into L2 (8B shape, 16 single tokens of 4000
+    // positions: 48.1 -> 44.0 us; of one row of 3000, three pages a warp, 8.5 -> 9.0, hence the bound.  With two CTAs per SM, hd 64, it costs 8 %.)
+    const bool ahead = HD == 128 && n_pages > 4 * p_step;
     for (int p = p_first, it = 0; p < n_pages; p += p_step, ++it) {
         if (it > 0 && (it & 31) == 0) id32 = ids(it);
         const int pg = __shfl_sync(0xffffffffu, id32, it & 31);
+        if (ahead) {
+            const int next = __shfl_sync(0xffffffffu, id32, (it + 1) & 31);
+            if (lane == 0 && ((it + 1) & 31) != 0 && p + p_step < n_pages && a.kv.holds(next)) {
+                l2_prefetch_bulk(a.kv.k + (size_t)next * page_stride + head_off, 16 * HD * 2);
+                l2_prefetch_bulk(a.kv.v + (size_t)next * page_stride + head_off, 16 * HD * 2);
+            }
+        }
         if (!a.kv.holds(pg)) continue;                          // (the same in every lane)
         const bf16 *kp = a.kv.k + (size_t)pg * page_stride + head_off, *vp = a.kv.v + (size_t)pg * page_stride + head_off;
         uint4 kf[2][KS];
