@@ -258,23 +258,26 @@ cudaError_t launch(const TreeArgs &a, int batch, int pages, cudaStream_t st) {
 
 cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
     const int pages = (max_len + a.max_nodes + 15) / 16;
-    // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 256 rows, but starts 2 to 3 us later.
-    // The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync / tcgen05, two kv layers in turn:
-    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions 7.8 /  9.4,  1000:  8.7 / 10.4,  4000: 14.6 / 14.4
-    //   8B shape, 4 x 8 nodes (64 tiles)     200           8.0 /  9.7,  1000: 11.2 / 12.3,  2000: 17.9 / 15.1,  4000: 27.8 /  22.1
-    //   13B shape, 1 x 26 nodes (80 tiles)   200           8.3 / 10.2,  1000: 14.4 / 14.1,  2000: 27.1 / 18.2,  4000: 45.6 /  26.8
-    //   1B shape, 8 x 8 nodes (128 tiles)    200           7.2 /  8.7,  1000:  9.8 / 13.1,  2000: 16.2 / 17.9,  4000: 25.1 /  26.8
-    //   8B shape, 4 x 33 nodes (288 tiles)                             1300: 37   / 19
-    //   8B shape, 4 x 64 nodes (512 tiles)    50          25.7 / 20.3
-    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 50.9 / 57.9), and two tiles of more units than the
-    // device has SMs go in one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 88 / 104).
+    // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 128 or 256 rows, but starts 1 to 3 us
+    // later.  The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync /
+    // tcgen05, two kv layers in turn:
+    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions  7.5 /  8.5,  1000:  8.3 /  9.5,  4000: 15.6 / 13.6,  30000: 73 / 45
+    //   8B shape, 4 x 8 nodes (64 tiles)     200            7.5 /  8.9,  1000: 10.9 / 10.9,  4000: 26.7 / 20.5
+    //   8B shape, 1 x 64 nodes (128 tiles)   100            7.9 / 10.4,  500:  11.7 / 11.3,  2000: 24.6 / 13.3
+    //   13B shape, 1 x 26 nodes (80 tiles)   200            8.0 /  9.4,  1000: 16.4 / 13.0,  4000: 43.4 / 24.6
+    //   8B shape, 4 x 33 nodes (288 tiles)   200           15.2 / 10.8,  1300: 36.0 / 17.8
+    //   1B shape, 1 x 32 nodes (64 tiles)    1000           8.6 /  9.3,  4000: 12.3 / 12.7,  8000: 19.2 / 16.4
+    //   1B shape, 4 x 16 nodes (128 tiles)   1000           9.4 / 10.0,  2000: 12.5 / 12.1,  8000: 39.2 / 25.7
+    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 46.4 / 56.8), and neither do two at head dimension 64,
+    // where an SM holds two CTAs (1B shape, 4 x 8 nodes, 8000: 24.1 / 25.0).  Two tiles of more units than the device has SMs go in
+    // one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 82 / 102).
     const int64_t tiles = ((int64_t)a.max_nodes * (a.nh / a.kv.nkv) + 15) / 16;
-    const int64_t units = (int64_t)a.kv.nkv * batch, tile_pages = units * tiles * pages * a.kv.hd / 128;
+    const int64_t units = (int64_t)a.kv.nkv * batch, tile_pages = units * tiles * pages;
     const int n_sms = current_sms();
     if (!n_sms) return cudaErrorInvalidDevice;
-    const bool waves = units * tiles > (a.kv.hd == 64 ? 2 : 1) * n_sms;      // (of mma.sync CTAs)
-    if (tiles > 1 && (waves || tile_pages > 6000) && !(tiles == 2 && units > n_sms))
-        return launch_tree_attention_tc(a, batch, max_len, st);
+    const bool wide = a.kv.hd == 128, waves = units * tiles > (wide ? 1 : 2) * n_sms;      // (of mma.sync CTAs)
+    const bool once = tiles == 1 || (tiles == 2 && (!wide || units > n_sms));
+    if (!once && (waves || tile_pages > (wide ? 4000 : 14000))) return launch_tree_attention_tc(a, batch, max_len, st);
     return a.kv.hd == 128 ? launch<128>(a, batch, pages, st) : launch<64>(a, batch, pages, st);
 }
 

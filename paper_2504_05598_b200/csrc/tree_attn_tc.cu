@@ -606,26 +606,55 @@ bool make_maps(const PageView &kv, Maps *m) {
               CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// how a call's blocks of keys are spread
+struct Plan {
+    int splits;          // CTAs of a cluster; 0: an error
+    int64_t steps;       // blocks that a CTA takes, times the waves of CTAs
+};
+
 template <int HD, int TILES>
-cudaError_t launch(const Maps &m, const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
+Plan plan(const TreeArgs &a, int batch, int max_len) {
     auto kern = tree_attention_tc_kernel<HD, TILES>;
     static SmemAttrOnce attr;
-    cudaError_t e = attr.set(kern, Cfg<HD, TILES>::SMEM);
-    if (e != cudaSuccess) return e;
-    const int group = a.nh / a.kv.nkv, n_rt = (a.max_nodes * group + TILES * BQ - 1) / (TILES * BQ);
-    // as many parts of the keys as are resident together, none for three blocks and less: joining parts costs as much as two blocks
     static ClusterRoom room;
-    const int blocks = (max_len + a.max_nodes + BKEY - 1) / BKEY;
-    const int splits = blocks <= 3 ? 1 : room.best(kern, Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, (int64_t)a.kv.nkv * n_rt * batch, blocks);
-    return launch_cluster(kern, dim3(splits, a.kv.nkv * n_rt, batch), Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, splits, st, m, a);
+    const int n_sms = current_sms();
+    if (!n_sms || attr.set(kern, Cfg<HD, TILES>::SMEM) != cudaSuccess) return Plan{0, 0};
+    // as many parts of the keys as are resident together, none for three blocks and less: joining parts costs as much as two blocks
+    const int n_rt = (a.max_nodes * (a.nh / a.kv.nkv) + TILES * BQ - 1) / (TILES * BQ), blocks = (max_len + a.max_nodes + BKEY - 1) / BKEY;
+    const int64_t units = (int64_t)a.kv.nkv * n_rt * batch;
+    const int splits = blocks <= 3 ? 1 : room.best(kern, Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, units, blocks);
+    return Plan{splits, (blocks + splits - 1) / splits * ((units * splits + n_sms - 1) / n_sms)};
+}
+
+template <int HD, int TILES>
+cudaError_t launch(const Maps &m, const TreeArgs &a, int batch, int splits, cudaStream_t st) {
+    const int n_rt = (a.max_nodes * (a.nh / a.kv.nkv) + TILES * BQ - 1) / (TILES * BQ);
+    return launch_cluster(tree_attention_tc_kernel<HD, TILES>, dim3(splits, a.kv.nkv * n_rt, batch), Cfg<HD, TILES>::THREADS, Cfg<HD, TILES>::SMEM, splits, st, m, a);
+}
+
+template <int HD>
+cudaError_t launch_form(const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
+    Maps m;
+    if (!make_maps(a.kv, &m)) return cudaErrorInvalidValue;
+    const Plan one = plan<HD, 1>(a, batch, max_len);
+    if (!one.splits) return cudaErrorInvalidDevice;
+    if (a.max_nodes * (a.nh / a.kv.nkv) > BQ) {
+        // Two tiles per CTA read the keys once for both, one's softmax beside the other's MMAs; with one per CTA (the second reads
+        // the keys from L2) there are twice the CTAs, with two score buffers each.  us, one / two tiles:
+        //   8B shape, 1 x 64 nodes   100 positions 10.4 / 17.8,  2000: 13.3 / 20.8,  16000:  41.9 /  49.6
+        //   8B shape, 4 x 64 nodes   500           13.8 / 19.2,  4000: 35.5 / 36.9,  16000: 106   /  90
+        //   8B shape, 8 x 64 nodes   1300          25.4 / 31.9,  4000: 58.0 / 57.2,  16000: 203   / 161
+        //   1B shape, 4 x 40 nodes   500           11.3 / 13.3,  4000: 27.3 / 26.4,  16000:  81   /  72
+        // That is 8.6 + 1.6 steps against 15.6 + 2.4 steps at head dimension 128, 8.4 + 1.15 against 10.5 + 2.0 at 64.
+        const Plan two = plan<HD, 2>(a, batch, max_len);
+        if (!two.splits) return cudaErrorInvalidDevice;
+        if (HD == 128 ? 3 * two.steps + 9 < 2 * one.steps : 7 * two.steps + 7 < 4 * one.steps) return launch<HD, 2>(m, a, batch, two.splits, st);
+    }
+    return launch<HD, 1>(m, a, batch, one.splits, st);
 }
 
 }  // namespace
 
 cudaError_t launch_tree_attention_tc(const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
-    Maps m;
-    if (!make_maps(a.kv, &m)) return cudaErrorInvalidValue;
-    const bool one = a.max_nodes * (a.nh / a.kv.nkv) <= BQ;
-    if (a.kv.hd == 128) return one ? launch<128, 1>(m, a, batch, max_len, st) : launch<128, 2>(m, a, batch, max_len, st);
-    return one ? launch<64, 1>(m, a, batch, max_len, st) : launch<64, 2>(m, a, batch, max_len, st);
+    return a.kv.hd == 128 ? launch_form<128>(a, batch, max_len, st) : launch_form<64>(a, batch, max_len, st);
 }
