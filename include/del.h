@@ -364,7 +364,7 @@ typedef struct {
  *   - products bf16 x bf16 with fp32 sums; softmax in fp32; probabilities rounded to bf16 for the product with the values. */
 typedef struct {
     const void *q;                /* bf16 [batch][max_nodes][n_heads][head_dim], rows q_node_stride apart, sequences q_seq_stride */
-    void *out, *out_lo;           /* bf16, like q; out_lo (may be null) gets the low part: out + out_lo carries 16 bits of mantissa */
+    void *out, *out_lo;           /* bf16, like q; out_lo (may be null) gets the low part: out + out_lo carries 16 bits of mantissa (0 where out is infinite) */
     const int32_t *page_table;    /* [batch] rows of table_cols entries, table_stride apart */
     const int32_t *lens, *nodes;  /* [batch]; nodes may be null: max_nodes everywhere */
     const uint64_t *mask;         /* [batch][max_nodes], may be null: a chain, node i sees nodes 0..i */

@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(THREADS, HD == 64 ? 2 : 1) tree_attention_kern
         const int i = rr / group, hq = rr - i * group;
         const size_t at = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD + c;
         uint32_t hi, lo;
-        split_bf16x2(o0 * inv, o1 * inv, hi, lo);
+        split_out(o0 * inv, o1 * inv, hi, lo);
         *reinterpret_cast<uint32_t *>(a.out + at) = hi;
         if (a.out_lo) *reinterpret_cast<uint32_t *>(a.out_lo + at) = lo;
     }

@@ -43,6 +43,13 @@ __device__ __forceinline__ bool sees(uint64_t bits, int tok, int len, int n_keys
     return tok < n_keys && (j < 0 || ((bits >> j) & 1));       // (n_keys - len <= 64)
 }
 
+// two outputs: packed high and low parts; where the high part is infinite the low one is zero (the difference would be no number)
+__device__ __forceinline__ void split_out(float x0, float x1, uint32_t &hi, uint32_t &lo) {
+    split_bf16x2(x0, x1, hi, lo);
+    if ((hi & 0x7fffu) == 0x7f80u) lo &= 0xffff0000u;
+    if ((hi & 0x7fff0000u) == 0x7f800000u) lo &= 0x0000ffffu;
+}
+
 }  // namespace tree
 
 // del_tree_attention behind its checks.  max_len: what lens are expected to reach.

@@ -499,10 +499,10 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {
                         uint4 hi, lo;
-                        split_bf16x2(__uint_as_float(o[e + 0]) * inv, __uint_as_float(o[e + 1]) * inv, hi.x, lo.x);
-                        split_bf16x2(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv, hi.y, lo.y);
-                        split_bf16x2(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv, hi.z, lo.z);
-                        split_bf16x2(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv, hi.w, lo.w);
+                        tree::split_out(__uint_as_float(o[e + 0]) * inv, __uint_as_float(o[e + 1]) * inv, hi.x, lo.x);
+                        tree::split_out(__uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv, hi.y, lo.y);
+                        tree::split_out(__uint_as_float(o[e + 4]) * inv, __uint_as_float(o[e + 5]) * inv, hi.z, lo.z);
+                        tree::split_out(__uint_as_float(o[e + 6]) * inv, __uint_as_float(o[e + 7]) * inv, hi.w, lo.w);
                         *reinterpret_cast<uint4 *>(a.out + out + c0 + e) = hi;
                         if (a.out_lo) *reinterpret_cast<uint4 *>(a.out_lo + out + c0 + e) = lo;
                     }
@@ -565,8 +565,8 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             const int rr = row0 + x, i = node_of(rr), hq = rr - i * group;
             const size_t at = b * a.o_seq + i * a.o_node + (size_t)(kvh * group + hq) * HD + 4 * c;
             uint2 hi, lo;
-            split_bf16x2(o.x, o.y, hi.x, lo.x);
-            split_bf16x2(o.z, o.w, hi.y, lo.y);
+            tree::split_out(o.x, o.y, hi.x, lo.x);
+            tree::split_out(o.z, o.w, hi.y, lo.y);
             *reinterpret_cast<uint2 *>(a.out + at) = hi;
             if (a.out_lo) *reinterpret_cast<uint2 *>(a.out_lo + at) = lo;
         }

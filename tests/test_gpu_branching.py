@@ -123,6 +123,32 @@ def test_what_is_masked_never_counts(nh, nkv, hd, n):
     check_tree(q, k, v, 2, table, lens, nodes, m)
 
 
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("batch", [12, 40])
+def test_many_sequences_of_many_rows(hd, batch):
+    """160 rows per kv head in so many sequences (most of them without nodes) that a CTA of the tcgen05 form takes two tiles: with the
+    keys in parts (12), and as a whole (40).  Slots that nobody sees and some drafted tokens hold no numbers, a page is named wrongly."""
+    n = 40
+    q, k, v, table, lens, nodes, m = make_tree(8, 2, hd, [0, 700, 35, 301] + [0] * (batch - 4), [n, n, n - 1, 17] + [0] * (batch - 4), n, seed=41)
+    m &= ~(1 << (n - 1))
+    m[:, 0] = 0
+    for b in range(4):
+        end = int(lens[b]) + int(nodes[b])
+        for p in range(end, -(-end // 16) * 16):
+            k[int(table[b, p // 16]), :, :, p % 16] = float("nan")
+            v[int(table[b, p // 16]), :, :, :, p % 16] = float("inf")
+        p = int(lens[b])
+        v[int(table[b, p // 16]), :, :, 5, p % 16] = float("-inf")
+        if n <= int(nodes[b]):
+            p = int(lens[b]) + n - 1
+            k[int(table[b, p // 16]), :, :, p % 16] = float("inf")
+            v[int(table[b, p // 16]), :, :, :, p % 16] = float("nan")
+    table[1, 20] = -1
+    q[3, 7, 6, 9] = float("nan")
+    check_tree(q, k, v, 2, table, lens, nodes, m)
+    check_tree(q, k, v, 1, table, lens, nodes, m, scale=0.4, low=True)
+
+
 @pytest.mark.parametrize("n", [1, 20])
 @pytest.mark.parametrize("hd", [64, 128])
 def test_no_number_stays_in_its_row(hd, n):
