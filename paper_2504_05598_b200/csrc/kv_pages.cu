@@ -18,7 +18,8 @@ namespace {
 // into shared memory, a lane picks the tokens of its dimensions in the order of their destinations and writes 32-byte rows (two bytes at a
 // time where a destination page is only partly written).  So values are read by whole source pages: of contexts kept by halves, 5
 // bytes move where 4 would do.  The copies are asynchronous and one round ahead, page ids two rounds, positions three: a round would
-// otherwise wait for three to five round trips to memory in turn (2 x 4 003 of 8 001 positions, 1B shape: 165 us that way).
+// otherwise wait for three to five round trips to memory in turn (2 x 4 003 of 8 001 positions, 1B shape: 165 us that way, 126 now:
+// 3900 GB/s of moved bytes, 4900 with the rest of the value pages).
 constexpr int CP_WARPS = 4, CP_RUNS = 2, CP_SPARSE = 4;      // source pages of a destination page that are staged, the next ones are loaded directly; with
                                                              // more than CP_SPARSE, each token's values are loaded by themselves
 
@@ -189,7 +190,8 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_kernel(const Compact
 }
 
 // The same for a few pages, one round of one part (accepted paths): nothing to pipeline, and the tokens of a page come from several
-// others.  A lane loads its dimensions' values of each token by themselves, all on their way together.
+// others.  A lane loads its dimensions' values of each token by themselves, all on their way together (4 paths of 5, 8B shape:
+// 6.5 to 7.3 us; through staged pages 14.6).
 template <int HD>
 __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_few_kernel(const CompactArgs a) {
     constexpr int KV = HD / 16, DPL = HD / 32;                  // 16-byte pieces of 16 keys, dimensions, per lane
@@ -247,6 +249,7 @@ __global__ void __launch_bounds__(CP_WARPS * 32, 4) compact_few_kernel(const Com
 //
 // One launch.  Which row gets which pages is a few hundred integers: every CTA works it out for itself in shared memory, and no CTA
 // waits for another.  Then the CTAs share the tables' rows and the pieces of the pages to copy; the last one lists the free pages.
+// 16 x 4 rows of the 8B shape: 15.9 us, 5000 GB/s; 1 x 4 rows of the 1B shape: 4.9 us, all latency.
 constexpr int FK_THREADS = 1024, FK_ROWS = 1024;
 constexpr int FK_MAX_FREE = 1 << 20;          // pages of which the used ones are marked in shared memory (128 KB of bits)
 constexpr int PIECE = 16384;                  // bytes of a page that a CTA copies at a time
