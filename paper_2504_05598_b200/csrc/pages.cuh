@@ -61,14 +61,12 @@ inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, i
     return cudaLaunchKernelEx(&cfg, kern, args...);
 }
 
-// How many clusters of `cluster_x` CTAs of a kernel the current device keeps resident, asked once per device and size (sizes 1..16,
-// `kept`: the caller's record per kernel).  A launch of more runs in waves: of clusters of 8 with one CTA per SM, B200 holds 15.
+// How many clusters of `cluster_x` CTAs (1..16) of a kernel a device keeps resident, asked once per device and size; one object per
+// kernel.  A launch of more runs in waves: of clusters of 8 with one CTA per SM, B200 holds 15.
 struct ClusterRoom {
     int n[DEL_MAX_DEVICES][17] = {};
     bool wide[DEL_MAX_DEVICES] = {};       // clusters of more than 8 are allowed for the kernel
-    template <typename K> int of(K kern, int threads, size_t smem, int cluster_x) {
-        int dev = 0;
-        if (cluster_x < 1 || cluster_x > 16 || cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEL_MAX_DEVICES) return 0;
+    template <typename K> int of(K kern, int threads, size_t smem, int cluster_x, int dev) {
         if (n[dev][cluster_x]) return n[dev][cluster_x];
         if (cluster_x > 8 && !wide[dev]) {
             if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
@@ -98,8 +96,10 @@ struct ClusterRoom {
     // together the one with the fewest steps per CTA, of equal ones the smallest.  Beyond 8 it pays where steps are many (one sequence of 30 000
     // positions, 8B shape: 10 CTAs per kv head 36.8 us, 8 CTAs 42.4; 1B shape 16 CTAs 22.9, 8 CTAs 35.3).
     template <typename K> int best(K kern, int threads, size_t smem, int64_t units, int steps) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= DEL_MAX_DEVICES) return 1;
         for (int c = steps < 16 ? steps : 16; c > 1; --c)
-            if (units <= of(kern, threads, smem, c)) {
+            if (units <= of(kern, threads, smem, c, dev)) {
                 const int each = (steps + c - 1) / c;
                 return (steps + each - 1) / each;
             }

@@ -57,7 +57,7 @@ struct Cfg {
     static constexpr uint32_t TMEM = 512;
     static_assert(O_BYTES <= RING, "outputs do not fit where the rings were");
     static_assert(O_COL + TILES * HD <= TMEM, "too much tensor memory");
-    static_assert(SMEM <= 232448 - 3072, "too much shared memory");
+    static_assert(SMEM <= 232448 - 4096, "too much shared memory");        // (beside the barriers and block maxima)
 };
 
 struct Maps { CUtensorMap k, v; };
