@@ -227,16 +227,35 @@ __global__ void __launch_bounds__(THREADS, HD == 64 ? 2 : 1) tree_attention_kern
         const int r = e / (HD / 2), c = (e - r * (HD / 2)) * 2, rr = mt * 16 + r;
         if (rr >= R) break;
         float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-        for (int k = 0; k < n_splits; ++k) m = fmaxf(m, (n_splits > 1 ? cl.map_shared_rank(tile_ml, k) : tile_ml)[r].x);
-        const float base = m == -INFINITY ? 0.f : m;
-        for (int k = 0; k < n_splits; ++k) {
-            const float2 ml = (n_splits > 1 ? cl.map_shared_rank(tile_ml, k) : tile_ml)[r];
-            const float *src = n_splits > 1 ? cl.map_shared_rank(&so[0][0][0], k) : &so[0][0][0];
-            const float2 v = *reinterpret_cast<const float2 *>(src + r * LD + c);
-            const float w = exp2f(ml.x - base);
-            l += ml.y * w;
-            o0 += v.x * w;
-            o1 += v.y * w;
+        if (n_splits == 1) {
+            const float2 v = *reinterpret_cast<const float2 *>(&so[0][r][c]);
+            l = tile_ml[r].y;
+            o0 = v.x;
+            o1 = v.y;
+        }
+#pragma unroll 1
+        for (int k0 = 0; n_splits > 1 && k0 < n_splits; k0 += 4) {            // states and outputs of four CTAs on their way together
+            float2 ml[4], v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                ml[k] = make_float2(-INFINITY, 0.f);
+                if (k0 + k < n_splits) {
+                    ml[k] = cl.map_shared_rank(tile_ml, k0 + k)[r];
+                    v[k] = *reinterpret_cast<const float2 *>(cl.map_shared_rank(&so[0][0][0], k0 + k) + r * LD + c);
+                }
+            }
+            const float m_new = fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)), base = m_new == -INFINITY ? 0.f : m_new;
+            const float f = exp2f(m - base);
+            m = m_new;
+            l *= f; o0 *= f; o1 *= f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k0 + k < n_splits) {
+                    const float w = exp2f(ml[k].x - base);
+                    l += ml[k].y * w;
+                    o0 += v[k].x * w;
+                    o1 += v[k].y * w;
+                }
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;             // nothing visible: zeros
         const int i = rr / group, hq = rr - i * group;
