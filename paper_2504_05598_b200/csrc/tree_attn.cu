@@ -284,16 +284,16 @@ cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cud
     // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 128 or 256 rows, but starts 1 to 3 us
     // later.  The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync /
     // tcgen05, two kv layers in turn:
-    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions  7.5 /  8.5,  1000:  8.3 /  9.5,  4000: 15.6 / 13.6,  30000: 73 / 45
-    //   8B shape, 4 x 8 nodes (64 tiles)     200            7.5 /  8.9,  1000: 10.9 / 10.9,  4000: 26.7 / 20.5
-    //   8B shape, 1 x 64 nodes (128 tiles)   100            7.9 / 10.4,  500:  11.7 / 11.3,  2000: 24.6 / 13.3
-    //   13B shape, 1 x 26 nodes (80 tiles)   200            8.0 /  9.4,  1000: 16.4 / 13.0,  4000: 43.4 / 24.6
-    //   8B shape, 4 x 33 nodes (288 tiles)   200           15.2 / 10.8,  1300: 36.0 / 17.8
-    //   1B shape, 1 x 32 nodes (64 tiles)    1000           8.6 /  9.3,  4000: 12.3 / 12.7,  8000: 19.2 / 16.4
-    //   1B shape, 4 x 16 nodes (128 tiles)   1000           9.4 / 10.0,  2000: 12.5 / 12.1,  8000: 39.2 / 25.7
-    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 46.4 / 56.8), and neither do two at head dimension 64,
-    // where an SM holds two CTAs (1B shape, 4 x 8 nodes, 8000: 24.1 / 25.0).  Two tiles of more units than the device has SMs go in
-    // one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 82 / 102).
+    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions  7.2 /  8.8,  1000:  8.1 /  9.5,  4000: 15.2 / 13.5,  30000: 73 / 45
+    //   8B shape, 4 x 8 nodes (64 tiles)     200            7.4 /  9.2,  1000: 10.5 / 10.9,  4000: 26.2 / 20.6
+    //   8B shape, 1 x 64 nodes (128 tiles)   100            7.1 / 10.3,  500:  10.8 / 11.3,  2000: 23.8 / 13.5
+    //   13B shape, 1 x 26 nodes (80 tiles)   200            7.2 /  9.7,  1000: 15.6 / 13.0,  4000: 42.6 / 24.8
+    //   8B shape, 4 x 33 nodes (288 tiles)   200           13.4 /  9.8,  1300: 34.5 / 17.9
+    //   1B shape, 1 x 32 nodes (64 tiles)    1000           8.0 /  9.1,  4000: 12.3 / 12.6,  8000: 19.0 / 16.4
+    //   1B shape, 4 x 16 nodes (128 tiles)   1000           9.2 /  9.9,  2000: 12.4 / 12.1,  8000: 38.8 / 25.6
+    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 45.4 / 57.8), and neither do two at head dimension 64,
+    // where an SM holds two CTAs (1B shape, 4 x 8 nodes, 8000: 23.8 / 25.0).  Two tiles of more units than the device has SMs go in
+    // one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 81 / 103).
     const int64_t tiles = ((int64_t)a.max_nodes * (a.nh / a.kv.nkv) + 15) / 16;
     const int64_t units = (int64_t)a.kv.nkv * batch, tile_pages = units * tiles * pages;
     const int n_sms = current_sms();
