@@ -3,11 +3,12 @@
 // For every sequence, kv head and tile of 16 query rows (node x query head of the group) one cluster of CTAs walks the pages of
 // the keys, each warp of it every so manyth page (so that the first page ids can be requested before the lengths are known).  A warp
 // keeps the online-softmax state of the tile in registers: S = Q K^T and O += P V are bf16 m16n8k16 MMAs with fp32 sums, the running
-// maximum and sum are fp32, the probabilities are rounded to bf16 for the second product.  The warps join through shared memory, the
-// CTAs of the cluster through distributed shared memory: one launch, no workspace, a fixed order of sums.
+// maximum and sum are fp32; the probabilities are rounded to bf16, which the MMA takes (off by 2^-8 of their value at most, as the
+// output's own rounding), their sum is of the unrounded ones.  The warps join through shared memory, the CTAs of the cluster through
+// distributed shared memory: one launch, no workspace, a fixed order of sums.
 //
 // Long calls are bound by HBM (single tokens, 8B shape, 16 rows of 4000 positions: 44 us, 5600 GB/s; 1B shape, 64 rows of 3000: 67 us,
-// 5480 GB/s), short ones by latency (8B shape, 8 nodes behind 200 positions: 7.1 us, of which an empty launch is some 2.5 and the walk
+// 5480 GB/s), short ones by latency (8B shape, 8 nodes behind 200 positions: 7.0 us, of which an empty launch is some 2.5 and the walk
 // lengths -> page ids -> keys -> join three round trips).
 //
 // Fragments: the MMA sums over its k index, so a permutation of k that both operands share is free.  For Q K^T a thread takes 16
