@@ -132,7 +132,7 @@ template <int HD, int TILES>
 __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_kernel(const __grid_constant__ Maps maps, const __grid_constant__ TreeArgs a) {
     using C = Cfg<HD, TILES>;
     extern __shared__ unsigned char smem_dyn[];
-    __shared__ __align__(8) uint64_t q_full, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], s_full[2], p_full[2], o_done[TILES], tile_bar, all_bar, pair_bar[TILES][4];
+    __shared__ __align__(8) uint64_t q_full, k_full[C::KS], k_empty[C::KS], v_full[C::VS], v_empty[C::VS], s_full[2], p_full[2], o_done[TILES], o_all[TILES], tile_bar, all_bar, pair_bar[TILES][4];
     __shared__ uint32_t tmem_base_s;
     __shared__ volatile int s_err;
     __shared__ int s_bad_page, s_odd[2];
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
             mbar_init(&s_full[i], 1);
             mbar_init(&p_full[i], 2 * (TILES == 2 ? max(1, quarters(i)) : quarters(0)));
         }
-        for (int t = 0; t < TILES; ++t) mbar_init(&o_done[t], 1);
+        for (int t = 0; t < TILES; ++t) { mbar_init(&o_done[t], 1); mbar_init(&o_all[t], 1); }
         s_err = 0;
         s_bad_page = s_odd[0] = s_odd[1] = 0;
         s_odd_tokens = 0;
@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                 umma_commit(&o_done[t]);
                 ++n_p[t];
                 if (t == n_tiles - 1) { umma_commit(&v_empty[j % C::VS]); n_v = j + 1; }
+                if (j == n_kb - 1) umma_commit(&o_all[t]);         // (last: nothing of this thread's arrives behind it)
                 return true;
             };
             for (int t = 0; ok && t < n_tiles; ++t) ok = scores(0, t, t);
@@ -309,7 +310,10 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                 for (int i = 0; i < 2; ++i)
                     if (n_s[i]) drain(&s_full[i], 1, 0, (uint32_t)n_s[i] & 1);
                 for (int t = 0; t < TILES; ++t)
-                    if (n_p[t]) drain(&o_done[t], 1, 0, (uint32_t)n_p[t] & 1);
+                    if (n_p[t]) {
+                        drain(&o_done[t], 1, 0, (uint32_t)n_p[t] & 1);
+                        if (n_p[t] == n_kb) drain(&o_all[t], 1, 0, 1);
+                    }
                 drain(k_empty, C::KS, n_k % C::KS, (uint32_t)(n_k / C::KS) & 1);
                 drain(v_empty, C::VS, n_v % C::VS, (uint32_t)(n_v / C::VS) & 1);
             }
@@ -422,7 +426,8 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                 }
                 l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
                 if (__any_sync(0xffffffffu, alpha != 1.f)) {
-                    // (the previous block's products are part of the output; with one tile they may still be running)
+                    // (The previous block's products are part of the output; with one tile they may still be running.  Those before them are done,
+                    // as this block's scores were issued after them, and this block's wait for this warp: the phase is the one meant.)
                     if (TILES == 1 && !wait_or_err(&o_done[t], (j - 1) & 1, &s_err)) { if (!s_err) s_err = 9; ok = false; break; }
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     for (int c0 = half * (HD / 2); c0 < (half + 1) * (HD / 2); c0 += 32) {
@@ -465,7 +470,10 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_full[buf]);
             }
-            if (ok && n_kb > 0 && !wait_or_err(&o_done[t], (n_kb - 1) & 1, &s_err)) { if (!s_err) s_err = 12; ok = false; }
+            // The output is complete: a barrier of its own, used once.  A wait names a phase of o_done by its parity alone, and here either of
+            // its last two phases may be open, or none: with one tile scores(j + 1) are issued before products(j), so the last
+            // scores say nothing about the products of the block before.
+            if (ok && n_kb > 0 && !wait_or_err(&o_all[t], 0, &s_err)) { if (!s_err) s_err = 12; ok = false; }
             if (half) s_sum[t][trow] = l;
             if (!meet(&all_bar, 1)) { if (!s_err) s_err = 13; ok = false; }       // both tiles are done with the rings, s_odd_tokens and the sums are complete
             l = half ? l : l + s_sum[t][trow];                   // (the first half's threads go on with the sum)
