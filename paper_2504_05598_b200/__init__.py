@@ -569,12 +569,13 @@ def _rows_of_heads(what: str, name: str, t, shape, dev: int):
 
 
 def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None, mask=None, out=None, out_lo=None,
-                   scale: Optional[float] = None, max_len: int = 0, stream=None):
+                   scale: Optional[float] = None, max_len: int = 0, stream=None, error=None):
     """del_tree_attention: attention of drafted trees (or single tokens) over a paged cache.
 
     q: bf16 [batch, nodes, heads, head_dim], the last two dimensions contiguous; page_table int32 [batch, columns]; lens, nodes int32
     [batch]; mask int64 [batch, nodes] (bit j of entry i: node i sees node j; None: a chain).  out (and out_lo, the low part of the result)
-    like q, made when None (on `stream`, whose work comes before any use of it); returns out.  max_len: what lens are expected to reach."""
+    like q, made when None (on `stream`, whose work comes before any use of it); returns out.  max_len: what lens are expected to reach.
+    error: int32 [1], set to a non-zero code if a bounded device-side wait ran out (the rows concerned are NaN either way), else left as it was."""
     what = "del_tree_attention"
     kv, _, hd, dev = _pages(what, k_pages, v_pages)
     shape = q.shape
@@ -598,7 +599,8 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
         if mask.dtype is not _t.int64 or mask.shape != (batch, n) or mask.get_device() != dev or not mask.is_contiguous():
             _refuse(what, "mask: contiguous int64 [batch, nodes] on the cache's device expected")
         mp = mask.data_ptr()
-    a = _PACK_TREE(qp, op, lp, tp, _vector(what, "lens", lens, batch, dev), np_, mp, 0, q_seq, q_node, o_seq, o_node, batch, n, nh, layer,
+    ep = 0 if error is None else _vector(what, "error", error, 1, dev)
+    a = _PACK_TREE(qp, op, lp, tp, _vector(what, "lens", lens, batch, dev), np_, mp, ep, q_seq, q_node, o_seq, o_node, batch, n, nh, layer,
                    cols, stride, max_len, scale or 0.0)
     _call(what, dev, (_lib or load_library()).del_tree_attention, kv, a, stream)
     return out

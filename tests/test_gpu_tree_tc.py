@@ -35,3 +35,29 @@ def test_one_tile_waits_for_all_of_its_products(nh, nkv, hd, n, batch, length):
     torch.cuda.synchronize()
     for out in outs:
         assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("nh,nkv,hd,n", [(4, 2, 64, 3), (40, 40, 128, 64)])
+def test_the_error_word_reaches_the_kernel(monkeypatch, nh, nkv, hd, n):
+    """A caller's word stays as it was where no wait runs out; it is the one the library is given; what is no such word is refused."""
+    q, k, v, table, lens, nodes, m = (t.cuda() for t in make_tree(nh, nkv, hd, [50], [n], n))
+    word = torch.tensor([0, 5, 0], dtype=torch.int32, device="cuda")
+    want = dl.tree_attention(q, k, v, 1, table, lens, nodes, m)
+    assert torch.equal(dl.tree_attention(q, k, v, 1, table, lens, nodes, m, error=word[1:2]), want)
+    assert word.tolist() == [0, 5, 0]
+    for bad in (word, word[1:2].float(), word[1:2].cpu(), word[:0]):
+        with pytest.raises(dl.DelError) as e:
+            dl.tree_attention(q, k, v, 1, table, lens, nodes, m, error=bad)
+        assert e.value.code == dl.EINVAL
+    given = []
+
+    class Library:
+        @staticmethod
+        def del_tree_attention(kv, args, stream):
+            given.append(dl.TreeAttnC.from_buffer_copy(args).error)
+            return dl.OK
+
+    monkeypatch.setattr(dl, "_lib", Library)
+    dl.tree_attention(q, k, v, 1, table, lens, nodes, m, error=word[1:2])
+    dl.tree_attention(q, k, v, 1, table, lens, nodes, m)
+    assert given == [word[1:2].data_ptr(), None]
