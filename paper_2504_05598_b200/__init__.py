@@ -577,6 +577,8 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
     like q, made when None (on `stream`, whose work comes before any use of it); returns out.  max_len: what lens are expected to reach.
     error: int32 [1], set to a non-zero code if a bounded device-side wait ran out (the rows concerned are NaN either way), else left as it was."""
     what = "del_tree_attention"
+    if scale is not None and not 2.0 ** -149 <= scale <= 2.0 ** 127:        # (0, also after rounding, is the C call's word for the default)
+        _refuse(what, "scale: a positive number that fp32 holds, or None for 1 / sqrt(head_dim), expected")
     kv, _, hd, dev = _pages(what, k_pages, v_pages)
     shape = q.shape
     if len(shape) != 4 or shape[3] != hd:
