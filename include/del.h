@@ -374,7 +374,7 @@ typedef struct {
     int32_t layer;                /* 1-based */
     int32_t table_cols, table_stride;
     int32_t max_len;              /* what lens are expected to reach (0: table_cols * 16): splits the work, changes no result but for the order of sums */
-    float scale;                  /* of the scores; 0: 1 / sqrt(head_dim) */
+    float scale;                  /* of the scores, scale * log2(e) finite in fp32; 0: 1 / sqrt(head_dim) */
 } del_tree_attn;
 int del_tree_attention(const del_pages *kv, const del_tree_attn *args, void *cuda_stream);
 

@@ -316,7 +316,7 @@ extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, v
     if (x->batch < 1 || x->batch > 65535 || x->max_nodes < 1 || x->max_nodes > 64) return DEL_EINVAL;
     if (x->n_heads < 1 || x->n_heads % a.kv.nkv || x->n_heads / a.kv.nkv > 1024 || x->layer < 1 || x->layer > a.kv.L) return DEL_EINVAL;
     if (x->table_cols < 1 || x->table_cols > (INT32_MAX - 1024) / 16 || x->table_stride < 0 || x->max_len < 0) return DEL_EINVAL;
-    if (!(x->scale >= 0.f && x->scale < INFINITY)) return DEL_EINVAL;
+    if (!(x->scale >= 0.f && x->scale * LOG2E < INFINITY)) return DEL_EINVAL;      // (the scores are powers of two)
     const int64_t group = x->n_heads / a.kv.nkv, tiles = (x->max_nodes * group + 15) / 16;
     if (tiles * a.kv.nkv > 65535) return DEL_EINVAL;
     a.q = (const bf16 *)x->q; a.out = (bf16 *)x->out; a.out_lo = (bf16 *)x->out_lo;
