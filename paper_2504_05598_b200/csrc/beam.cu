@@ -495,16 +495,16 @@ cudaError_t launch(const BeamArgs &a, cudaStream_t st) {
     cfg.gridDim = dim3(a.slices, a.b.batch * a.b.beams);
     if (a.fused) {
         static SmemAttrOnce attr;
-        static bool big[DEL_MAX_DEVICES] = {};
+        static std::atomic<bool> big[DEL_MAX_DEVICES] = {};
         auto kern = beam_slice_kernel<T, true>;
         cudaError_t e = attr.set(kern, (int)(fixed + Cand::bytes(MAX_CLUSTER * MAX_K)));
         int dev = 0;
         if (e == cudaSuccess) e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
-        if (a.slices * a.b.beams > 8 && !(dev < DEL_MAX_DEVICES && big[dev])) {
+        if (a.slices * a.b.beams > 8 && !(dev < DEL_MAX_DEVICES && big[dev].load(std::memory_order_acquire))) {
             e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
             if (e != cudaSuccess) return e;
-            if (dev < DEL_MAX_DEVICES) big[dev] = true;
+            if (dev < DEL_MAX_DEVICES) big[dev].store(true, std::memory_order_release);
         }
         at[1].id = cudaLaunchAttributeClusterDimension;
         at[1].val.clusterDim.x = a.slices;

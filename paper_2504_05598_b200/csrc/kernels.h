@@ -1,20 +1,22 @@
 // Internal launch interface between the host-side round scheduler (del_api.cu) and the kernels.
 #pragma once
 
+#include <atomic>
+
 #include "common.cuh"
 
 // cudaFuncSetAttribute acts on the current device only: a kernel's dynamic shared-memory limit is raised once per
 // device (a process may drive contexts on several GPUs).  `done` is the caller's static per-kernel record.
 #define DEL_MAX_DEVICES 64
 struct SmemAttrOnce {
-    bool done[DEL_MAX_DEVICES] = {};
+    std::atomic<bool> done[DEL_MAX_DEVICES] = {};              // (several threads may come at once, and set the same)
     template <typename K> cudaError_t set(K kern, int bytes) {
         int dev = 0;
         cudaError_t e = cudaGetDevice(&dev);
         if (e != cudaSuccess) return e;
-        if (dev >= 0 && dev < DEL_MAX_DEVICES && done[dev]) return cudaSuccess;
+        if (dev >= 0 && dev < DEL_MAX_DEVICES && done[dev].load(std::memory_order_acquire)) return cudaSuccess;
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e == cudaSuccess && dev >= 0 && dev < DEL_MAX_DEVICES) done[dev] = true;
+        if (e == cudaSuccess && dev >= 0 && dev < DEL_MAX_DEVICES) done[dev].store(true, std::memory_order_release);
         return e;
     }
 };

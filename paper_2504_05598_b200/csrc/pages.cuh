@@ -1,6 +1,8 @@
 // Device view of a paged cache handed to the context-free operators (del_pages), and the launch helper they share.
 #pragma once
 
+#include <atomic>
+
 #include "../../include/del.h"
 #include "kernels.h"
 
@@ -28,13 +30,13 @@ cudaError_t launch_kv_compact(const PageView &kv, const del_compact &x, cudaStre
 
 // SMs of the current device (0: the query failed)
 inline int current_sms() {
-    static int n[DEL_MAX_DEVICES] = {};
+    static std::atomic<int> n[DEL_MAX_DEVICES] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    if (dev >= 0 && dev < DEL_MAX_DEVICES && n[dev]) return n[dev];
-    int sms = 0;
+    int sms = dev >= 0 && dev < DEL_MAX_DEVICES ? n[dev].load(std::memory_order_relaxed) : 0;
+    if (sms) return sms;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    if (dev >= 0 && dev < DEL_MAX_DEVICES) n[dev] = sms;
+    if (dev >= 0 && dev < DEL_MAX_DEVICES) n[dev].store(sms, std::memory_order_relaxed);
     return sms;
 }
 
@@ -62,18 +64,20 @@ inline cudaError_t launch_cluster(K kern, dim3 grid, int threads, size_t smem, i
 }
 
 // How many clusters of `cluster_x` CTAs (1..16) of a kernel a device keeps resident, asked once per device and size; one object per
-// kernel.  A launch of more runs in waves: of clusters of 8 with one CTA per SM, B200 holds 15.
+// kernel.  A launch of more runs in waves: of clusters of 8 with one CTA per SM, B200 holds 15.  (Several threads may ask at once, and
+// write the same values.)
 struct ClusterRoom {
-    int n[DEL_MAX_DEVICES][17] = {};
-    bool wide[DEL_MAX_DEVICES] = {};       // clusters of more than 8 are allowed for the kernel
+    std::atomic<int> n[DEL_MAX_DEVICES][17] = {};
+    std::atomic<bool> wide[DEL_MAX_DEVICES] = {};       // clusters of more than 8 are allowed for the kernel
     template <typename K> int of(K kern, int threads, size_t smem, int cluster_x, int dev) {
-        if (n[dev][cluster_x]) return n[dev][cluster_x];
-        if (cluster_x > 8 && !wide[dev]) {
+        int got = n[dev][cluster_x].load(std::memory_order_acquire);
+        if (got) return got;
+        if (cluster_x > 8 && !wide[dev].load(std::memory_order_acquire)) {
             if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
                 cudaGetLastError();
                 return 0;
             }
-            wide[dev] = true;
+            wide[dev].store(true, std::memory_order_release);
         }
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(cluster_x);
@@ -85,12 +89,12 @@ struct ClusterRoom {
         at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         cfg.attrs = at;
         cfg.numAttrs = 1;
-        int got = 0;
         if (cudaOccupancyMaxActiveClusters(&got, kern, &cfg) != cudaSuccess) {
             cudaGetLastError();
             return 0;
         }
-        return n[dev][cluster_x] = got;
+        n[dev][cluster_x].store(got, std::memory_order_release);
+        return got;
     }
     // Cluster size (1: none) for `units` clusters with `steps` steps of work each: of those sizes whose clusters are all resident
     // together the one with the fewest steps per CTA, of equal ones the smallest.  Beyond 8 it pays where steps are many (one sequence of 30 000
