@@ -1071,6 +1071,9 @@ double exit_threshold(del_ctx *c, int sq, int E) {
     return t;
 }
 
+// a sequence of `positions` that may emit max_new tokens more, the rows of a last round behind them
+bool fits(const del_ctx *c, int positions, int max_new) { return (int64_t)positions + max_new + c->sh.g_max + 1 <= c->D.max_seq; }
+
 int clip_gamma(const SeqHost &s, int gamma) { return std::max(0, std::min(gamma, s.remaining - 1)); }
 
 bool seq_ok(const del_ctx *c, int sq) { return c && sq >= 0 && sq < c->D.B; }
@@ -1256,7 +1259,7 @@ int del_prefill(del_ctx *c, int sq, const int32_t *prompt, int n_prompt, int max
     c->in_round = false;
     for (int i = 0; i < n_prompt; ++i)
         if (prompt[i] < 0 || prompt[i] >= c->D.V) return DEL_EINVAL;
-    if (n_prompt + max_new_tokens + c->sh.g_max + 1 > c->D.max_seq) return DEL_ENOSPC;
+    if (!fits(c, n_prompt, max_new_tokens)) return DEL_ENOSPC;
     release_seq(c, sq);
     SeqHost &s = c->seq[sq];
     int rc = ensure_pages(c, sq, n_prompt + 1);
@@ -1631,7 +1634,7 @@ int del_fork(del_ctx *c, int from, int to, int max_new_tokens) {
     const SeqHost &src = c->seq[from];
     if (!src.active || src.phase != 0) return DEL_ESTATE;
     const Dims &D = c->D;
-    if (src.T + max_new_tokens + c->sh.g_max + 1 > D.max_seq) return DEL_ENOSPC;
+    if (!fits(c, src.T, max_new_tokens)) return DEL_ENOSPC;
     const int full = src.T / 16, part = src.T % 16;
     {
         // a page of its own for the part-filled last one, from the free ones or from what `to` holds alone
