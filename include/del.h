@@ -177,7 +177,9 @@ int del_round(del_ctx *ctx, del_round_out *out);
  * feed (parents[i] = -1); 0 <= n_drafts < DEL_MAX_ROWS.  A node sees the committed positions and its ancestors, and is rotated by its
  * depth.  Greedy: starting at the root, the target's top-1 token is emitted, and the walk goes on at the child that carries it (of
  * several the first).  The keys and values of the path are moved together and committed.  out_tokens (HOST int32 [n_drafts + 1]) gets
- * the n_emitted tokens: at least 1, at most the depth of the tree + 1 and what is left of max_new_tokens.  Statistics and the choice of the next
+ * the n_emitted tokens: at least 1, at most the depth of the tree + 1 and what is left of max_new_tokens.  Drafts too deep for what is left take no
+ * part; the others and the root need as many positions behind the committed ones (with a max_seq of
+ * prompt + max_new_tokens + 63 every tree fits to the end; the pages stay with the sequence), else DEL_ENOSPC and nothing changes.  Statistics and the choice of the next
  * (E, gamma), which are about drafts of the exit layers, stay as they are; rounds of both kinds may follow one another.  Synchronises.
  * Errors: DEL_EINVAL, DEL_ESTATE (no prefill, finished, a round half done, or the slot samples), DEL_ENOSPC, DEL_ETIMEOUT. */
 int del_verify_tree(del_ctx *ctx, int seq, int n_drafts, const int32_t *tokens, const int32_t *parents, int32_t *out_tokens,

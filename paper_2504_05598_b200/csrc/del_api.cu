@@ -1541,27 +1541,32 @@ int del_verify_tree(del_ctx *c, int sq, int n_drafts, const int32_t *tokens, con
     *n_emitted = 0;
     if (!s.active || s.remaining < 1 || s.phase != 0 || samples(c, sq)) return DEL_ESTATE;
     const Dims &D = c->D;
-    const int n = n_drafts + 1;                                   // node 0: the token that the next round feeds
-    int rc = ensure_pages(c, sq, s.T + n);
-    if (rc) return rc;
-    // what each node sees, its depth
+    // The nodes of the pass: 0 is the token that the next round feeds, then the drafts that can still be emitted (the others lie deeper
+    // than what is left of max_new_tokens, and so does all that follows them): token, parent, depth, what it sees.
     TreeDev *t = reinterpret_cast<TreeDev *>(reinterpret_cast<char *>(c->stage_host) + 40960);
-    int depth[DEL_ROWS_MAX];
+    int32_t *tok = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(c->stage_host) + 49152);
+    int node[DEL_ROWS_MAX], depth[DEL_ROWS_MAX], parent[DEL_ROWS_MAX], n = 1;      // node: of a draft, -1: left out
     t->mask[0] = 1;
     depth[0] = 0;
-    for (int i = 1; i < n; ++i) {
-        t->mask[i] = t->mask[parents[i - 1] + 1] | (1ull << i);
-        depth[i] = depth[parents[i - 1] + 1] + 1;
+    for (int i = 0; i < n_drafts; ++i) {
+        const int up = parents[i] < 0 ? 0 : node[parents[i]];
+        node[i] = up < 0 || depth[up] + 1 >= s.remaining ? -1 : n;
+        if (node[i] < 0) continue;
+        t->mask[n] = t->mask[up] | (1ull << n);
+        depth[n] = depth[up] + 1;
+        parent[n] = up;
+        tok[n - 1] = tokens[i];
+        ++n;
     }
+    int rc = ensure_pages(c, sq, s.T + n);
+    if (rc) return rc;
     t->len = s.T;
     t->nodes = n;
     CK(cudaMemcpyAsync(c->tree_dev, t, offsetof(TreeDev, src_pos), cudaMemcpyHostToDevice, c->st));
     c->h2d_bytes += offsetof(TreeDev, src_pos);
-    if (n_drafts) {
-        int32_t *tok = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(c->stage_host) + 49152);
-        memcpy(tok, tokens, sizeof(int32_t) * n_drafts);
-        CK(cudaMemcpyAsync(c->B.TOK + (size_t)sq * (D.S + 1) + 1, tok, sizeof(int32_t) * n_drafts, cudaMemcpyHostToDevice, c->st));
-        c->h2d_bytes += sizeof(int32_t) * n_drafts;
+    if (n > 1) {
+        CK(cudaMemcpyAsync(c->B.TOK + (size_t)sq * (D.S + 1) + 1, tok, sizeof(int32_t) * (n - 1), cudaMemcpyHostToDevice, c->st));
+        c->h2d_bytes += sizeof(int32_t) * (n - 1);
     }
     c->in_round = true;
     rc = plan_begin(c, 1);
@@ -1606,7 +1611,7 @@ int del_verify_tree(del_ctx *c, int sq, int n_drafts, const int32_t *tokens, con
         ++k;
         int next = -1;
         for (int i = n - 1; i > cur; --i)
-            if (parents[i - 1] + 1 == cur && tokens[i - 1] == got[cur]) next = i;
+            if (parent[i] == cur && tok[i - 1] == got[cur]) next = i;
         if (next < 0 || k == s.remaining) break;
         cur = next;
     }

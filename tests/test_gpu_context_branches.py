@@ -20,3 +20,46 @@ def test_token_counts_are_added_in_64_bits():
     ctx.fork(0, 1, 19)
     assert ctx.committed_len(1) == len(prompt)
     ctx.close()
+
+
+@pytest.mark.parametrize("n", [15, 63])
+def test_trees_up_to_the_last_token(n):
+    """With the positions that a generation of the library's own drafts needs and no more, trees that reach far past the last token are verified up to it."""
+    dl, cfg, ctx, prompt = make(TINY_GQA, gen=48, max_seq=TINY_GQA.max_seq)
+    want, margins = plain_stream(ctx, 0, prompt, 48)
+    rng = np.random.default_rng(n)
+    out = ctx.prefill(1, prompt, 48).emitted()
+    while len(out) < 48:
+        left = 48 - len(out)
+        if left < 20:                                            # a chain, right for some steps, and then a tree that follows it
+            good = want[len(out):]
+            good = good[:int(rng.integers(0, 5))]
+            tokens = [int(t) for t in good] + [int(t) for t in rng.integers(0, cfg.vocab, n - len(good))]
+            parents = [i - 1 if i <= left else int(rng.integers(left, i)) for i in range(n)]
+            got, expect = ctx.verify_tree(1, tokens, parents), min(len(good) + 1, left)
+        else:
+            got, expect = ctx.verify_tree(1, [], []), 1
+        if not agrees(got, want, margins, len(out)):
+            break
+        assert expect <= len(got) <= left
+        out += got
+    assert len(out) > 40
+    if len(out) == 48:
+        with pytest.raises(dl.DelError) as e:
+            ctx.verify_tree(1, [1], [-1])
+        assert e.value.code == dl.ESTATE
+    ctx.close()
+
+
+def test_drafts_that_are_left_out_do_not_count():
+    """A draft too deep to be emitted, and what follows it, may stand anywhere in the list: the others give what they give without it."""
+    dl, cfg, ctx, prompt = make(TINY_GQA, gen=30)
+    want, margins = plain_stream(ctx, 0, prompt, 30)
+    ctx.prefill(1, prompt, 4)                                    # three tokens are left: drafts of depth 1 and 2 can be emitted
+    a, b, c = (int(t) for t in want[1:4])
+    wrong = (a + 1) % cfg.vocab
+    tokens, parents = [wrong, 5, 6, a, 7, 8, b, 9, c, 10], [-1, 0, 1, -1, 2, 3, 3, 5, 6, 7]
+    got = ctx.verify_tree(1, tokens, parents)
+    if agrees(got, want, margins, 1):
+        assert got == [a, b, c]
+    ctx.close()
