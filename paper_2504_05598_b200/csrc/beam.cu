@@ -11,9 +11,14 @@
 // maxima, r = k / 4 of them; the k-th of all listed is a bar that at least k logits reach and, for logits in no special order, hardly
 // more.  What reaches the bar goes to a list; every four chunks the list is ranked by counting where it has grown, and its k-th
 // becomes the bar.  A logit that passes costs a warp some 250 cycles, so the bar has to be good: with the smallest of the warps'
-// maxima as the first bar (54 logits of 8192 pass instead of k) 16 x 8 x 128256 took 84 us, 45 of them for what passed.  Where the list would
+// maxima as the first bar (54 logits of 8192 pass instead of k) 16 x 8 x 128256 took 84 us, 45 of them for what passed.  Behind the first
+// chunk a logit has to lie above the bar, as an equal one has a higher token.  Where the list would
 // overflow (rising logits, say) the k largest of the four chunks are taken one by one.  What is left per logit is its load, a
 // maximum, a comparison, an exponential and a sum.
+//
+// Equal logits cost more in a slice's first chunk, where all of them pass to the comparison of keys: with all but 10 tokens of each row at
+// -inf, 16 x 8 x 128256 takes 36 us instead of 24 (87 when equal ones passed in every chunk), 4 x 4 of 128256 in bf16 47 instead of 15,
+// 1 x 4 x 32000 24 instead of 7.7; rows of one value 43, 57 and 29.  With more allowed tokens in a chunk than k nothing changes.
 //
 // The smallest calls are all latency, much of it instruction fetch: what runs rarely reads the logits again in rolled loops instead of
 // unrolling over the registers that hold them.
@@ -50,6 +55,8 @@ __device__ __forceinline__ uint32_t ordered(float x) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+// the next number above (of +inf: none, nothing is below it)
+__device__ __forceinline__ float above(float x) { return unordered(ordered(x) + 1); }
 __device__ __forceinline__ u64 make_key(float x, int token) { return ((u64)ordered(x) << 32) | (0xffffffffu - (uint32_t)token); }
 __device__ __forceinline__ int key_token(u64 key) { return (int)(0xffffffffu - (uint32_t)key); }
 __device__ __forceinline__ float key_value(u64 key) { return unordered((uint32_t)(key >> 32)); }
@@ -291,6 +298,7 @@ __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int 
                 }
             }
         }
+        if (c0 == lo && bar) bar_x = above(bar_x);                // (from here on a logit that equals the bar has a higher token)
     };
     // after a group of chunks: did the list hold, and can the bar be raised?
     auto look = [&](int g0) __attribute__((always_inline)) {
@@ -303,7 +311,7 @@ __device__ __forceinline__ int slice_best(Shared &sm, const T *row, int lo, int 
             count = prune(count, k);
             if (count == k) {
                 bar = sm.list[k - 1];
-                bar_x = key_value(bar);
+                bar_x = above(key_value(bar));
             }
             // (prune's last barrier lies between these reads and the next writes to the list: they go behind its k entries)
         }
