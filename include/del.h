@@ -399,11 +399,12 @@ int del_kv_compact(const del_pages *kv, const del_compact *args, void *cuda_stre
  * lens[a], full pages are shared, and a part-filled last page stays with the lowest b of the parent while the others get copies in
  * spare pages.  Then each row gets pages for `room` more positions (within new_cols).  Spare pages are taken in order,
  * rows ascending, a row's copy first.  parents[b] outside [0, n_old): the row is given up, new_lens[b] = 0, no page.
- *   - entries of new_table behind a row's pages are left as they were; new_table and new_lens must not overlap table and lens;
+ *   - entries of new_table behind a row's pages are left as they were; what is written (new_table, new_lens, free_pages, counts) must not
+ *     overlap what is read, nor one another;
  *   - spare (n_spare[0] <= spare_cap ids, DEVICE): pages that no row holds.  Where they run out, or where the parent's or the spare page's
  *     id is outside [0, n_pages), the entry becomes -1 and counts[1] goes up by one;
  *   - free_pages (may be null): the ids in [0, n_pages) that no new row holds, ascending, counts[0] of them, the rest of the array
- *     left as it was; it holds n_pages entries, may not overlap spare, and serves as the next call's spare with n_spare = counts.
+ *     left as it was; it holds n_pages entries and serves as the next call's spare with n_spare = counts.
  *   - lens below 0 count as 0, and are cut to what the rows of both tables hold; shared entries are passed on as they are.
  * 1 <= n_old, n_new <= 1024; n_new * new_cols < 2^31; with free_pages n_pages <= 1 << 20. */
 typedef struct {

@@ -446,9 +446,16 @@ extern "C" int del_kv_fork(const del_pages *kv, const del_fork_args *x, void *cu
     if (x->old_stride < x->old_cols || x->new_stride < x->new_cols || x->spare_cap < 0 || x->room < 0) return DEL_EINVAL;
     if (x->free_pages && a.kv.n_pages > FK_MAX_FREE) return DEL_EINVAL;
     const size_t old_bytes = 4 * ((size_t)(x->n_old - 1) * x->old_stride + x->old_cols), new_bytes = 4 * ((size_t)(x->n_new - 1) * x->new_stride + x->new_cols);
-    if (overlap(x->table, old_bytes, x->new_table, new_bytes) || overlap(x->lens, 4 * (size_t)x->n_old, x->new_lens, 4 * (size_t)x->n_new)) return DEL_EINVAL;
-    if (x->free_pages && overlap(x->free_pages, 4 * (size_t)a.kv.n_pages, x->spare, 4 * (size_t)x->spare_cap)) return DEL_EINVAL;
-    if (overlap(x->counts, 8, x->n_spare, 4)) return DEL_EINVAL;        // the count is read by CTAs that may start after the last one is done
+    // nothing is written that is read, or written twice: CTAs may start after others are done
+    struct Range { const void *p; size_t n; };
+    const Range in[] = {{x->table, old_bytes}, {x->lens, 4 * (size_t)x->n_old}, {x->parents, 4 * (size_t)x->n_new}, {x->spare, 4 * (size_t)x->spare_cap}, {x->n_spare, 4}};
+    const Range out[] = {{x->new_table, new_bytes}, {x->new_lens, 4 * (size_t)x->n_new}, {x->counts, 8}, {x->free_pages, x->free_pages ? 4 * (size_t)a.kv.n_pages : 0}};
+    for (int i = 0; i < 4; ++i) {
+        for (const Range &r : in)
+            if (overlap(out[i].p, out[i].n, r.p, r.n)) return DEL_EINVAL;
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return DEL_EINVAL;
+    }
     const int n_sms = current_sms();
     if (!n_sms) return DEL_ECUDA;
     a.f = *x;
