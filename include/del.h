@@ -401,7 +401,7 @@ int del_kv_compact(const del_pages *kv, const del_compact *args, void *cuda_stre
  * rows ascending, a row's copy first.  parents[b] outside [0, n_old): the row is given up, new_lens[b] = 0, no page.
  *   - entries of new_table behind a row's pages are left as they were; what is written (new_table, new_lens, free_pages, counts) must not
  *     overlap what is read, nor one another;
- *   - spare (n_spare[0] <= spare_cap ids, DEVICE): pages that no row holds.  Where they run out, or where the parent's or the spare page's
+ *   - spare (n_spare[0] <= spare_cap ids, DEVICE; may be null if spare_cap is 0): pages that no row holds.  Where they run out, or where the parent's or the spare page's
  *     id is outside [0, n_pages), the entry becomes -1 and counts[1] goes up by one;
  *   - free_pages (may be null): the ids in [0, n_pages) that no new row holds, ascending, counts[0] of them, the rest of the array
  *     left as it was; it holds n_pages entries and serves as the next call's spare with n_spare = counts.

@@ -436,7 +436,7 @@ extern "C" int del_kv_compact(const del_pages *kv, const del_compact *x, void *c
 extern "C" int del_kv_fork(const del_pages *kv, const del_fork_args *x, void *cuda_stream) {
     ForkArgs a;
     if (!x || !page_view(kv, &a.kv)) return DEL_EINVAL;
-    if (!x->table || !x->lens || !x->parents || !x->spare || !x->n_spare || !x->new_table || !x->new_lens || !x->counts) return DEL_EINVAL;
+    if (!x->table || !x->lens || !x->parents || (!x->spare && x->spare_cap) || !x->n_spare || !x->new_table || !x->new_lens || !x->counts) return DEL_EINVAL;
     if (((uintptr_t)x->table | (uintptr_t)x->lens | (uintptr_t)x->parents | (uintptr_t)x->spare | (uintptr_t)x->n_spare | (uintptr_t)x->new_table |
          (uintptr_t)x->new_lens | (uintptr_t)x->free_pages | (uintptr_t)x->counts) & 3)
         return DEL_EINVAL;
