@@ -363,7 +363,9 @@ typedef struct {
  *   - a row that sees nothing gets zeros; output rows i >= nodes[b] are left as they were;
  *   - masked positions never contribute, whatever their pages hold; positions behind the table's columns or on a page id outside
  *     [0, n_pages) are masked; lens and nodes below 0 count as 0, nodes above max_nodes as max_nodes;
- *   - products bf16 x bf16 with fp32 sums; softmax in fp32; probabilities rounded to bf16 for the product with the values. */
+ *   - products bf16 x bf16 with fp32 sums; softmax in fp32; probabilities rounded to bf16 (each off by 2^-8 of itself at most) for the product
+ *     with the values: out_lo carries the sums' further bits, not the probabilities';
+ *   - out and out_lo must not overlap q. */
 typedef struct {
     const void *q;                /* bf16 [batch][max_nodes][n_heads][head_dim], rows q_node_stride apart, sequences q_seq_stride */
     void *out, *out_lo;           /* bf16, like q; out_lo (may be null) gets the low part: out + out_lo carries 16 bits of mantissa (0 where out is infinite) */
@@ -375,7 +377,8 @@ typedef struct {
     int32_t batch, max_nodes, n_heads;       /* max_nodes 1..64, n_heads a multiple (up to 1024) of n_kv_heads, batch 1..65535 */
     int32_t layer;                /* 1-based */
     int32_t table_cols, table_stride;
-    int32_t max_len;              /* what lens are expected to reach (0: table_cols * 16): splits the work, changes no result but for the order of sums */
+    int32_t max_len;              /* what lens are expected to reach (0: table_cols * 16): picks the kernel and how its work is split.  Results are the same
+                                   * within the rounding of the probabilities and the order of sums, and the same bits for the same call, max_len and table_cols */
     float scale;                  /* of the scores, scale * log2(e) finite in fp32; 0: 1 / sqrt(head_dim) */
 } del_tree_attn;
 int del_tree_attention(const del_pages *kv, const del_tree_attn *args, void *cuda_stream);

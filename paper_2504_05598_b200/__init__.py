@@ -574,8 +574,9 @@ def tree_attention(q, k_pages, v_pages, layer: int, page_table, lens, nodes=None
 
     q: bf16 [batch, nodes, heads, head_dim], the last two dimensions contiguous; page_table int32 [batch, columns]; lens, nodes int32
     [batch]; mask int64 [batch, nodes] (bit j of entry i: node i sees node j; None: a chain).  out (and out_lo, the low part of the result)
-    like q, made when None (on `stream`, whose work comes before any use of it); returns out.  max_len: what lens are expected to reach.
-    error: int32 [1], set to a non-zero code if a bounded device-side wait ran out (the rows concerned are NaN either way), else left as it was."""
+    like q, made when None (on `stream`, whose work comes before any use of it); returns out; neither may overlap q.  max_len: what
+    lens are expected to reach (picks the kernel and how its work is split).  error: int32 [1], set to a non-zero code if a bounded
+    device-side wait ran out (the rows concerned are NaN either way), else left as it was."""
     what = "del_tree_attention"
     if scale is not None and not 2.0 ** -149 <= scale <= 2.0 ** 127:        # (0, also after rounding, is the C call's word for the default)
         _refuse(what, "scale: a positive number that fp32 holds, or None for 1 / sqrt(head_dim), expected")

@@ -521,12 +521,6 @@ __global__ void __launch_bounds__(Cfg<HD, TILES>::THREADS, 1) tree_attention_tc_
                     }
                 }
             }
-            if (n_splits == 1 && n_kb == 0 && row_ok) {             // a table of no position at all
-                for (int e = 0; e < HD; e += 8) {
-                    *reinterpret_cast<uint4 *>(a.out + out + e) = make_uint4(0, 0, 0, 0);
-                    if (a.out_lo) *reinterpret_cast<uint4 *>(a.out_lo + out + e) = make_uint4(0, 0, 0, 0);
-                }
-            }
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         }
     }
