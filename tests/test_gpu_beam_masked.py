@@ -62,3 +62,12 @@ def test_masked_rows_cost_little_more():
         return best
 
     assert ms(masked) < 3 * ms(x)
+
+
+@pytest.mark.parametrize("batch,beams,vocab,k,dtype", [(4, 4, 128257, 8, torch.float32), (4, 4, 128257, 8, torch.bfloat16), (4, 4, 50257, 8, torch.float16),
+                                                       (12, 8, 50257, 16, torch.float32), (12, 8, 50257, 16, torch.float16)])
+def test_rows_of_odd_length_at_size(batch, beams, vocab, k, dtype):
+    """Rows that start anywhere between 16-byte boundaries, in one launch and in two, slices of several chunks."""
+    g = torch.Generator().manual_seed(vocab + k)
+    logits = (2.5 * torch.randn(batch, beams, vocab, generator=g)).to(dtype)
+    check_beam(logits, -10 * torch.rand(batch, beams, generator=g), k, torch.rand(batch, beams, generator=g) < 0.1, 2)

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import synth
 from cases import TINY_GQA
 from test_gpu_tree_rounds import agrees, make, plain_stream, random_tree
 
@@ -62,4 +63,39 @@ def test_drafts_that_are_left_out_do_not_count():
     got = ctx.verify_tree(1, tokens, parents)
     if agrees(got, want, margins, 1):
         assert got == [a, b, c]
+    ctx.close()
+
+
+# heads whose trees of 49 nodes and more take the tcgen05 form of the tree attention in every layer (four tiles of 16 rows for each of them do
+# not fit the device at once), at either head dimension
+WIDE = [synth.small_variant(TINY_GQA, name="wide_hd128", n_layers=3, n_heads=40, n_kv_heads=40, head_dim=128, e_max=2, seed=91),
+        synth.small_variant(TINY_GQA, name="wide_hd64", n_layers=3, n_heads=80, n_kv_heads=80, head_dim=64, e_max=2, seed=92)]
+
+
+@pytest.mark.parametrize("cfg", WIDE, ids=lambda c: c.name)
+@pytest.mark.parametrize("flags", ["default", "streaming head", "tcgen05 layers"])
+def test_wide_trees_on_tcgen05_emit_the_plain_stream(cfg, flags):
+    """Rounds whose attention runs on tcgen05 between the layer GEMMs of either form; with 16 nodes now and then, which take the other form."""
+    dl, cfg, ctx, prompt = make(cfg, gen=80)
+    if flags == "streaming head":
+        ctx.set_flags(dl.FLAG_PDL)
+    elif flags == "tcgen05 layers":
+        ctx.set_flags(dl.FLAG_PDL | dl.FLAG_TC | dl.FLAG_TC_ROWS_ALL)
+    want, margins = plain_stream(ctx, 0, prompt, 80)
+    rng = np.random.default_rng(5)
+    out, most, rounds = ctx.prefill(1, prompt, 80).emitted(), 0, 0
+    while len(out) < 80:
+        n = (63, 48, 16, 55)[rounds % 4]
+        tokens, parents, depth = random_tree(rng, n, want[len(out):], cfg.vocab, 0.2)
+        if rounds % 5 == 4:
+            got, expect = ctx.round()[1].emitted(), None
+        else:
+            got, expect = ctx.verify_tree(1, tokens, parents), min(depth + 1, 80 - len(out))
+        if not agrees(got, want, margins, len(out)):
+            break
+        assert expect is None or len(got) >= expect
+        assert ctx.committed_len(1) == len(prompt) + len(out) + len(got) - 1
+        most, rounds = max(most, len(got)), rounds + 1
+        out += got
+    assert rounds > 3 and most > 3, (rounds, most)
     ctx.close()
