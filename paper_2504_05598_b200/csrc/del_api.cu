@@ -476,7 +476,7 @@ int run_layer(del_ctx *c, const PassInfo &pi, int l, bool write_exit, bool first
         TreeArgs a = *tree;
         a.layer = l;
         TAG(CLS_ATTN, 4.0 * pi.max_kv * D.nkv * D.hd);
-        LAUNCH(launch_tree_attention(a, 1, pi.max_kv, c->st));
+        LAUNCH(launch_tree_attention(a, 1, pi.max_kv, c->st, !wt));
     } else {
         AttnArgs a;
         memset(&a, 0, sizeof(a));

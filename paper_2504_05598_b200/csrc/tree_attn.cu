@@ -22,6 +22,7 @@
 #include <cstring>
 
 #include "tree_attn.cuh"
+#include "tree_form.h"
 
 namespace cg = cooperative_groups;
 
@@ -280,28 +281,10 @@ cudaError_t launch(const TreeArgs &a, int batch, int pages, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st) {
-    const int pages = (max_len + a.max_nodes + 15) / 16;
-    // Which form: tiles of 16 rows on mma.sync walk the pages once each, the tcgen05 form once for 128 or 256 rows, but starts 1 to 3 us
-    // later.  The line is drawn by the tile-pages of the call, and where the tiles do not fit the device at once.  us, mma.sync /
-    // tcgen05, two kv layers in turn:
-    //   8B shape, 1 x 16 nodes (32 tiles)    200 positions  7.2 /  8.8,  1000:  8.1 /  9.5,  4000: 15.2 / 13.5,  30000: 73 / 45
-    //   8B shape, 4 x 8 nodes (64 tiles)     200            7.4 /  9.2,  1000: 10.5 / 10.9,  4000: 26.2 / 20.6
-    //   8B shape, 1 x 64 nodes (128 tiles)   100            7.1 / 10.3,  500:  10.8 / 11.3,  2000: 23.8 / 13.5
-    //   13B shape, 1 x 26 nodes (80 tiles)   200            7.2 /  9.7,  1000: 15.6 / 13.0,  4000: 42.6 / 24.8
-    //   8B shape, 4 x 33 nodes (288 tiles)   200           13.4 /  9.8,  1300: 34.5 / 17.9
-    //   1B shape, 1 x 32 nodes (64 tiles)    1000           8.0 /  9.1,  4000: 12.3 / 12.6,  8000: 19.0 / 16.4
-    //   1B shape, 4 x 16 nodes (128 tiles)   1000           9.2 /  9.9,  2000: 12.4 / 12.1,  8000: 38.8 / 25.6
-    // A single tile reads nothing twice (8B shape, 16 x 4 nodes, 4000 positions: 45.4 / 57.8), and neither do two at head dimension 64,
-    // where an SM holds two CTAs (1B shape, 4 x 8 nodes, 8000: 23.8 / 25.0).  Two tiles of more units than the device has SMs go in
-    // one wave of small CTAs where the other form needs two (13B shape, 4 x 17 nodes, 4000: 81 / 103).
-    const int64_t tiles = ((int64_t)a.max_nodes * (a.nh / a.kv.nkv) + 15) / 16;
-    const int64_t units = (int64_t)a.kv.nkv * batch, tile_pages = units * tiles * pages;
-    const int n_sms = current_sms();
+cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st, bool streaming) {
+    const int pages = (max_len + a.max_nodes + 15) / 16, n_sms = current_sms();
     if (!n_sms) return cudaErrorInvalidDevice;
-    const bool wide = a.kv.hd == 128, waves = units * tiles > (wide ? 1 : 2) * n_sms;      // (of mma.sync CTAs)
-    const bool once = tiles == 1 || (tiles == 2 && (!wide || units > n_sms));
-    if (!once && (waves || tile_pages > (wide ? 4000 : 14000))) return launch_tree_attention_tc(a, batch, max_len, st);
+    if (tree::takes_tcgen05(a.kv.hd, a.kv.nkv, a.nh / a.kv.nkv, a.max_nodes, batch, pages, n_sms, streaming)) return launch_tree_attention_tc(a, batch, max_len, st);
     return a.kv.hd == 128 ? launch<128>(a, batch, pages, st) : launch<64>(a, batch, pages, st);
 }
 
@@ -326,5 +309,5 @@ extern "C" int del_tree_attention(const del_pages *kv, const del_tree_attn *x, v
     a.scale = (x->scale > 0.f ? x->scale : 1.f / sqrtf((float)a.kv.hd)) * LOG2E;
     a.err = x->error;
     const int len = x->max_len ? (x->max_len < x->table_cols * 16 ? x->max_len : x->table_cols * 16) : x->table_cols * 16;
-    return launch_tree_attention(a, x->batch, len, (cudaStream_t)cuda_stream) == cudaSuccess ? DEL_OK : DEL_ECUDA;
+    return launch_tree_attention(a, x->batch, len, (cudaStream_t)cuda_stream, false) == cudaSuccess ? DEL_OK : DEL_ECUDA;
 }

@@ -52,7 +52,7 @@ __device__ __forceinline__ void split_out(float x0, float x1, uint32_t &hi, uint
 
 }  // namespace tree
 
-// del_tree_attention behind its checks.  max_len: what lens are expected to reach.
-cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st);
+// del_tree_attention behind its checks.  max_len: what lens are expected to reach; streaming: register-streaming GEMMs run around it (tree_form.h).
+cudaError_t launch_tree_attention(const TreeArgs &a, int batch, int max_len, cudaStream_t st, bool streaming);
 // Tiles of up to 256 query rows on tcgen05 (tree_attn_tc.cu)
 cudaError_t launch_tree_attention_tc(const TreeArgs &a, int batch, int max_len, cudaStream_t st);

@@ -66,9 +66,10 @@ def test_drafts_that_are_left_out_do_not_count():
     ctx.close()
 
 
-# heads whose trees of 49 nodes and more take the tcgen05 form of the tree attention in every layer (four tiles of 16 rows for each of them do
-# not fit the device at once), at either head dimension
+# heads whose trees of 49 nodes and more take the tcgen05 form of the tree attention in every layer, as four tiles of 16 rows for each of them
+# do not fit the device at once (head dimension 128: between tcgen05 layer GEMMs; between streaming ones behind 4000 positions)
 WIDE = [synth.small_variant(TINY_GQA, name="wide_hd128", n_layers=3, n_heads=40, n_kv_heads=40, head_dim=128, e_max=2, seed=91),
+        synth.small_variant(TINY_GQA, name="wide_hd128_long", n_layers=3, n_heads=40, n_kv_heads=40, head_dim=128, e_max=2, prompt_len=4100, seed=93),
         synth.small_variant(TINY_GQA, name="wide_hd64", n_layers=3, n_heads=80, n_kv_heads=80, head_dim=64, e_max=2, seed=92)]
 
 
