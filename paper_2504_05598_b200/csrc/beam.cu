@@ -544,8 +544,15 @@ int slices_of(const del_beam &x, int n_sms) {
     return n < 1 ? 1 : (int)n;
 }
 
-// The one-launch form: slices per row such that an item is a cluster, all of which are resident, and no slice is longer than what
-// a second launch costs (about 32768 columns, 6 us); 0: two launches
+// The one-launch form: slices per row such that an item is a cluster, all of which are resident (B200: 15 of 8, 7 of 16), and no slice is
+// longer than 32768 columns; 0: two launches, which spread the rows over more CTAs.  us on the device, one launch / two:
+//                    1 x 4 fp32    1 x 4 bf16    2 x 4 fp32    2 x 4 bf16    4 x 4 fp32    4 x 4 bf16    7 x 4 fp32    7 x 4 bf16    1 x 8 fp32    4 x 8 bf16
+//   vocab  32000      8.4 / 10.2    9.5 / 11.0    8.8 /  9.7   11.5 / 10.9    8.8 /  9.5   14.7 / 11.6    9.0 /  9.9   14.8 / 17.2   12.8 / 12.0   22.2 / 12.1
+//          64128      9.4 / 11.6    9.3 / 12.5    9.7 / 11.5   13.1 / 13.2    9.9 /  9.6   13.1 / 11.5   10.0 / 10.8   14.8 / 17.4   14.7 / 14.3   24.0 / 12.2
+//         128256     11.3 / 13.3   12.4 / 14.7   11.5 / 11.6   16.1 / 13.3   11.8 / 10.5   14.5 / 11.0   12.0 / 12.7   16.4 / 18.2   18.7 / 14.4   27.1 / 14.0
+//         262144     14.2 / 13.3   15.0 / 14.6   14.7 / 12.8   16.5 / 13.0   14.8 / 12.7   18.5 / 13.1   15.6 / 16.5   19.0 / 21.1   24.1 / 15.6   32.2 / 17.8
+// A second launch costs the host up to 4 us more where nothing else runs (1 x 4 x 8000: 8.6 us a call / 12.6).  The line is right for one
+// to four beams of few items and errs to one launch where 4 items of 4 beams or any of 8 would have more CTAs in two (in 16 bits by 3 to 12 us).
 int fused_slices(const del_beam &x) {
     if (x.beams > MAX_CLUSTER) return 0;
     const int most = (x.vocab + 2047) / 2048, n = MAX_CLUSTER / x.beams < most ? MAX_CLUSTER / x.beams : most;

@@ -105,7 +105,9 @@ struct ClusterRoom {
         for (int c = steps < 16 ? steps : 16; c > 1; --c)
             if (units <= of(kern, threads, smem, c, dev)) {
                 const int each = (steps + c - 1) / c, least = (steps + each - 1) / each;
-                return least == 3 && c > 3 ? 4 : least;           // (3 are slower than 4: 8B shape, 500 positions 9.1 us against 7.8)
+                // (3 are slower than 4 or as fast: 8B shape, 16 nodes behind 500 positions 8.2 / 7.5 us, behind 700 8.3 / 8.0, 2 x 8 nodes
+                // behind 700 8.2 / 7.9, 3 x 4 nodes 7.9 / 7.4; 120 other calls of both forms, 300 to 4000 positions, within 3 %)
+                return least == 3 && c > 3 ? 4 : least;
             }
         return 1;
     }

@@ -13,7 +13,10 @@
 // Shared memory's 128 bytes per clock are what the MMAs compete for: with N = 64 and P in shared memory, scores and products of a
 // block of 64 keys read 80 KB per tile (640 cycles, 256 of arithmetic); with N = 128 and P in tensor memory 48 KB.
 // Roles: warp 0 issues the copies, warp 1 the MMAs, eight warps per tile do the softmax; quarters of a tile without rows do nothing.
-// With two tiles each has one score buffer and one tile's softmax runs beside the other's MMAs; a single tile has two buffers.
+// With two tiles each has one score buffer and one tile's softmax runs beside the other's MMAs; a single tile has two buffers.  (Two buffers of
+// 128 keys for each of two tiles would take 2 x 2 x 128 + 2 x 128 = 768 columns of tensor memory at head dimension 128; of 64 keys 512, all there are.)
+// Registers: the 18 warps of two tiles count as 20, which leaves 96 a thread, and the softmax spills (68 bytes stored, 92 loaded at head
+// dimension 128, 228 and 248 at 64); with one tile 144 and 167 a thread, no spills.
 // What bounds it (8B shape): 8 x 64 nodes over 32.7k positions 302 to 314 us, 3250 GB/s and 840 TFLOP/s, half of either rate: a tile's
 // softmax waits for its scores and its products for the softmax, and the two tiles' chains (2.3 us per block) overlap in part.
 // One sweep by the reference maximum so far, repeated where it did not hold, scores 16 at a time with the next on their way, was
